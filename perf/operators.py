@@ -327,7 +327,7 @@ def _own_lookup(st):
         return st["out"]
     ams.ams_dedup(st["ids"], c["rows"], st["uniq"], st["inv"], st["perm"], st["off"], st["n_uniq"], st["status"],
                   st["ws"])
-    ams.ams_lookup_bwd(st["uniq"], st["perm"], st["off"], st["n_uniq"], c["n"], st["dout"], st["grad"], st["ws"],
+    ams.ams_lookup_bwd(st["uniq"], st["inv"], st["perm"], st["off"], st["n_uniq"], c["n"], st["dout"], st["grad"], st["ws"],
                        st["scale"], st["pad_id"])
     return st["out"], st["uniq"][:st["n_u"]], st["grad"][:st["n_u"]]
 
