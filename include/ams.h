@@ -505,6 +505,39 @@ ams_status ams_adam_update(int64_t n, float *param, const float *grad, float *m,
                            float lr, float b1, float b2, float eps, int64_t t,
                            uint16_t *param_bf16, void *stream);
 
+/* ================================================ sequence operators ====
+ * Behavior lists as token sequences: rows of an embedding table per token
+ * (ams_bag_fwd keeps only their sum), and multi-head attention of a sample's
+ * queries to its own list.  `dtype` is AMS_F32 or AMS_BF16 (else DTYPE), the
+ * storage of the rows that go in and come out; sums, softmax statistics and
+ * the row gradients of a table are float32.  Row strides (ld_*) are in elements. */
+
+/* ------------------------------------------------------------ lookup ----
+ * out[k][d] = scale * table[ids[k]][d]   for k < n, d < D (1 <= D <= 65536).
+ * ids [n] (device); table [n_rows x D] with row stride ld_table >= D; out
+ * [n x D] with row stride ld_out >= D.  A token whose ID is pad_id (a negative
+ * pad_id: none) or outside [0, n_rows) gets a zero row.  bf16: the float32
+ * product is rounded once.  out must not overlap table.
+ * bwd:  the merged gradient of the touched rows, from the tokens' sorted order
+ *       (uniq, inv, occ_perm, uniq_off, n_uniq of ams_dedup over ids):
+ *         grad[u][d] = scale * sum over the tokens k of uniq[u] of dout[k][d],
+ *       zero for uniq[u] == pad_id; grad [n_uniq_cap x D] float32, written for
+ *       u < n_u (what ams_adagrad_rows takes).  dout [n x D] in dtype, row
+ *       stride ld_dout >= D.  A row's tokens are added in an order that depends
+ *       on n and on their places in the sorted order alone.
+ *       ws: at least ams_lookup_workspace(n, D) bytes; that size also serves
+ *       every smaller n.
+ * Host errors: DTYPE, DIMS (D), SIZE (n outside [0, 2^30 - 1], n_rows < 0, a
+ * stride below D, n_uniq_cap < 0), NULL, WORKSPACE. */
+ams_status ams_lookup_fwd(int32_t dtype, int32_t D, float scale, int32_t pad_id, const int32_t *ids, int64_t n,
+                          const void *table, int64_t n_rows, int64_t ld_table, void *out, int64_t ld_out,
+                          void *stream);
+size_t ams_lookup_workspace(int64_t n, int32_t D);
+ams_status ams_lookup_bwd(int32_t dtype, int32_t D, float scale, int32_t pad_id, int64_t n, const int32_t *uniq,
+                          const int32_t *inv, const int32_t *occ_perm, const int32_t *uniq_off,
+                          const int32_t *n_uniq, int32_t n_uniq_cap, const void *dout, int64_t ld_dout, float *grad,
+                          void *ws, size_t ws_bytes, void *stream);
+
 /* ============================================================= probes ====
  * Achievable-peak probes of the device (they compute nothing of the method):
  * the rates the part delivers for plain HBM streams, for gathering table

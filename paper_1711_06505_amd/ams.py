@@ -28,7 +28,7 @@ EXPORTS = ["ams_status_str", "ams_build_info", "ams_dedup_workspace", "ams_dedup
            "ams_bag_fwd", "ams_bag_workspace", "ams_bag_bwd", "ams_ctr_workspace", "ams_ctr_fwd_bwd",
            "ams_adagrad_rows", "ams_pool_query_fwd", "ams_pool_query_bwd",
            "ams_adam_update", "ams_pool_concat_fwd", "ams_pool_concat_bwd", "ams_dssm_workspace",
-           "ams_dssm_fwd_bwd", "ams_peak_copy", "ams_peak_read", "ams_peak_gather", "ams_peak_mfma"]
+           "ams_dssm_fwd_bwd", "ams_lookup_fwd", "ams_lookup_workspace", "ams_lookup_bwd", "ams_peak_copy", "ams_peak_read", "ams_peak_gather", "ams_peak_mfma"]
 
 
 class AmsError(RuntimeError):
@@ -116,6 +116,12 @@ def load() -> ctypes.CDLL:
     f = ctypes.c_float
     lib.ams_adam_update.restype = ctypes.c_int
     lib.ams_adam_update.argtypes = [i64, P, P, P, P, f, f, f, f, i64, P, P]
+    lib.ams_lookup_fwd.restype = ctypes.c_int
+    lib.ams_lookup_fwd.argtypes = [i32, i32, f, i32, P, i64, P, i64, i64, P, i64, P]
+    lib.ams_lookup_workspace.restype = sz
+    lib.ams_lookup_workspace.argtypes = [i64, i32]
+    lib.ams_lookup_bwd.restype = ctypes.c_int
+    lib.ams_lookup_bwd.argtypes = [i32, i32, f, i32, i64, P, P, P, P, P, i32, P, i64, P, P, sz, P]
     for name, args in (("ams_peak_copy", [P, P, i64, i32, P]), ("ams_peak_read", [P, i64, i32, P, P]),
                        ("ams_peak_gather", [P, i64, i32, P, i32, i32, P, i32, P, P]),
                        ("ams_peak_mfma", [i32, P, i32, i32, P, P])):
@@ -380,6 +386,105 @@ def ams_adagrad_rows(uniq, n_uniq, n_uniq_cap: int, grad, table, accum, lr: floa
     _check(load().ams_adagrad_rows(table.shape[1], _p(uniq), _p(n_uniq), int(n_uniq_cap), _p(grad), _p(table),
                                    table.shape[0], _p(accum), float(lr), float(eps), _stream(stream)),
            "ams_adagrad_rows")
+
+
+# --------------------------------------------------- sequence operators
+
+_STORAGE = {torch.float32: AMS_F32, torch.bfloat16: AMS_BF16}
+
+
+class _Call:
+    """Checks of one call's tensors (ValueError), then the call itself on the
+    tensors' device and the given or current stream there."""
+
+    def __init__(self, where: str):
+        self.where, self.device = where, None
+
+    def _same_device(self, name, t):
+        if t.device.type != "cuda":
+            raise ValueError(f"{self.where}: {name} is on {t.device}, not on a GPU")
+        if self.device is None:
+            self.device = t.device
+        elif t.device != self.device:
+            raise ValueError(f"{self.where}: {name} is on {t.device}, other arguments on {self.device}")
+
+    def vec(self, name, t, dtype, least: int):
+        """A contiguous tensor of at least `least` elements."""
+        if t.dtype != dtype:
+            raise ValueError(f"{self.where}: {name} must be {dtype}, not {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{self.where}: {name} must be contiguous")
+        if t.numel() < least:
+            raise ValueError(f"{self.where}: {name} has {t.numel()} elements, {least} needed")
+        self._same_device(name, t)
+        return _p(t)
+
+    def rows(self, name, t, dtype, n: int, inner):
+        """Rows of `inner` (contiguous within a row), at least n of them;
+        returns (pointer, row stride)."""
+        if t.dtype != dtype:
+            raise ValueError(f"{self.where}: {name} must be {dtype}, not {t.dtype}")
+        if tuple(t.shape[1:]) != tuple(inner) or t.shape[0] < n:
+            raise ValueError(f"{self.where}: {name} is {tuple(t.shape)}, [{n}, {', '.join(map(str, inner))}] needed")
+        width = 1
+        for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+            if size > 1 and stride != width:
+                raise ValueError(f"{self.where}: a row of {name} must be contiguous")
+            width *= size
+        if t.shape[0] > 1 and t.stride(0) < width:
+            raise ValueError(f"{self.where}: the rows of {name} overlap")
+        self._same_device(name, t)
+        return _p(t), max(t.stride(0), width) if t.shape[0] > 1 else width
+
+    def storage(self, name, t) -> int:
+        if t.dtype not in _STORAGE:
+            raise ValueError(f"{self.where}: {name} must be float32 or bfloat16, not {t.dtype}")
+        return _STORAGE[t.dtype]
+
+    def run(self, f, *args, stream=None):
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        elif stream.device != self.device:
+            raise ValueError(f"{self.where}: a stream of {stream.device}, tensors on {self.device}")
+        if self.device.index == torch.cuda.current_device():
+            rc = f(*args, ctypes.c_void_p(stream.cuda_stream))
+        else:
+            with torch.cuda.device(self.device):
+                rc = f(*args, ctypes.c_void_p(stream.cuda_stream))
+        _check(rc, self.where)
+
+
+def ams_lookup_fwd(ids, table, out, scale: float = 1.0, pad_id: int = -1, stream=None):
+    """out[k] = scale * table[ids[k]] (float32 or bfloat16 rows, any row stride)."""
+    c = _Call("ams_lookup_fwd")
+    n, D = ids.numel(), table.shape[1]
+    dt = c.storage("table", table)
+    ip = c.vec("ids", ids, torch.int32, n)
+    tp, ldt = c.rows("table", table, table.dtype, 0, (D,))
+    op, ldo = c.rows("out", out, table.dtype, n, (D,))
+    c.run(load().ams_lookup_fwd, dt, D, float(scale), int(pad_id), ip, n, tp, table.shape[0], ldt, op, ldo,
+          stream=stream)
+
+
+def ams_lookup_workspace(n: int, D: int) -> int:
+    return load().ams_lookup_workspace(int(n), int(D))
+
+
+def ams_lookup_bwd(uniq, inv, occ_perm, uniq_off, n_uniq, n_uniq_cap: int, dout, grad, ws, scale: float = 1.0,
+                   pad_id: int = -1, stream=None):
+    """grad[u] = scale * the sum of dout over the tokens of uniq[u], from the
+    outputs of ams_dedup over the tokens' IDs (dout has one row per token)."""
+    c = _Call("ams_lookup_bwd")
+    n, D = dout.shape
+    dt, i32 = c.storage("dout", dout), torch.int32
+    dp, ldd = c.rows("dout", dout, dout.dtype, n, (D,))
+    args = [c.vec("uniq", uniq, i32, min(n, n_uniq_cap)), c.vec("inv", inv, i32, n),
+            c.vec("occ_perm", occ_perm, i32, n), c.vec("uniq_off", uniq_off, i32, min(n, n_uniq_cap) + 1),
+            c.vec("n_uniq", n_uniq, i32, 1)]
+    gp = c.vec("grad", grad, torch.float32, min(n, n_uniq_cap) * D)
+    wp = c.vec("ws", ws, torch.uint8, 0)
+    c.run(load().ams_lookup_bwd, dt, D, float(scale), int(pad_id), n, *args, int(n_uniq_cap), dp, ldd, gp, wp,
+          ws.numel(), stream=stream)
 
 
 # ---------------------------------------------------------------- probes
