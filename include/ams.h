@@ -538,6 +538,52 @@ ams_status ams_lookup_bwd(int32_t dtype, int32_t D, float scale, int32_t pad_id,
                           const int32_t *n_uniq, int32_t n_uniq_cap, const void *dout, int64_t ld_dout, float *grad,
                           void *ws, size_t ws_bytes, void *stream);
 
+/* --------------------------------------------------- cross attention ----
+ * Multi-head attention of each sample's queries (say, candidate ads) to that
+ * sample's keys (its behavior states), lists of their own lengths.
+ * For query head h of query i of a sample, key head h / (n_heads / n_kv_heads):
+ *   s_j = scale * <q_i, k_j>, w = softmax_j(s_j) over the sample's keys that
+ *   key_mask keeps, out_i = sum_j w_j v_j; a query without such a key gets a
+ *   zero row, and lse = -infinity. */
+typedef struct {
+    int32_t dtype;       /* AMS_F32 or AMS_BF16: q, k, v, out and their gradients */
+    int32_t n_heads;     /* query heads, 1..4096 */
+    int32_t n_kv_heads;  /* key and value heads; divides n_heads */
+    int32_t head_dim;    /* 1..128 */
+    float scale;         /* of the scores */
+} ams_attn;
+
+/* fwd:  q_off [B+1], k_off [B+1] CSR offsets (device) of the samples' queries
+ *       and keys, non-decreasing within [0, n_q] and [0, n_k]; rows that no
+ *       sample owns are neither read nor written.
+ *       q, out [n_q x n_heads x head_dim], k, v [n_k x n_kv_heads x head_dim],
+ *       row strides ld_* >= the heads' width.  k and v may be the same array.
+ *       key_mask [n_k] bytes, or NULL: a key whose byte is 0 takes no part,
+ *       whatever its k and v rows hold (NaN included).
+ *       lse [n_q x n_heads] out, or NULL for inference: ln sum_j e^(s_j).
+ * bwd:  the same inputs, the forward's out and lse, and dout [n_q x n_heads x
+ *       head_dim]; dq, dk, dv like q, k, v: fully overwritten on the samples'
+ *       rows (zero for masked keys and for queries without keys, whose dout is
+ *       not used), other rows left as they were.  k and v being one array, the
+ *       gradient is dk + dv.  dq, dk, dv must not overlap anything.
+ * Arithmetic: float32 products and sums for AMS_F32; for AMS_BF16 exact bf16
+ *       products with float32 sums, the softmax in float32, and one rounding to
+ *       bf16 of the weights (of their gradients) before the second product.
+ * ws:   at least ams_xattn_workspace(attn, B, n_q, n_k) bytes, for either call.
+ * Host errors: NULL, DTYPE, DIMS (heads, head_dim), SIZE (a negative size,
+ * n_q * n_heads / n_kv_heads or n_k above 2^31 - 1, a stride below the width,
+ * more than 2^24 - 1 tiles of 16 rows or 64 keys in all), WORKSPACE. */
+size_t ams_xattn_workspace(const ams_attn *attn, int32_t B, int64_t n_q, int64_t n_k);
+ams_status ams_xattn_fwd(const ams_attn *attn, int32_t B, const int32_t *q_off, int64_t n_q, const int32_t *k_off,
+                         int64_t n_k, const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v,
+                         int64_t ld_v, const uint8_t *key_mask, void *out, int64_t ld_out, float *lse, void *ws,
+                         size_t ws_bytes, void *stream);
+ams_status ams_xattn_bwd(const ams_attn *attn, int32_t B, const int32_t *q_off, int64_t n_q, const int32_t *k_off,
+                         int64_t n_k, const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v,
+                         int64_t ld_v, const uint8_t *key_mask, const void *out, int64_t ld_out, const float *lse,
+                         const void *dout, int64_t ld_dout, void *dq, int64_t ld_dq, void *dk, int64_t ld_dk,
+                         void *dv, int64_t ld_dv, void *ws, size_t ws_bytes, void *stream);
+
 /* ============================================================= probes ====
  * Achievable-peak probes of the device (they compute nothing of the method):
  * the rates the part delivers for plain HBM streams, for gathering table

@@ -28,7 +28,8 @@ EXPORTS = ["ams_status_str", "ams_build_info", "ams_dedup_workspace", "ams_dedup
            "ams_bag_fwd", "ams_bag_workspace", "ams_bag_bwd", "ams_ctr_workspace", "ams_ctr_fwd_bwd",
            "ams_adagrad_rows", "ams_pool_query_fwd", "ams_pool_query_bwd",
            "ams_adam_update", "ams_pool_concat_fwd", "ams_pool_concat_bwd", "ams_dssm_workspace",
-           "ams_dssm_fwd_bwd", "ams_lookup_fwd", "ams_lookup_workspace", "ams_lookup_bwd", "ams_peak_copy", "ams_peak_read", "ams_peak_gather", "ams_peak_mfma"]
+           "ams_dssm_fwd_bwd", "ams_lookup_fwd", "ams_lookup_workspace", "ams_lookup_bwd",
+           "ams_xattn_workspace", "ams_xattn_fwd", "ams_xattn_bwd", "ams_peak_copy", "ams_peak_read", "ams_peak_gather", "ams_peak_mfma"]
 
 
 class AmsError(RuntimeError):
@@ -48,6 +49,11 @@ class ams_mlp(ctypes.Structure):
 
 class ams_ctr(ctypes.Structure):
     _fields_ = [("n_layers", ctypes.c_int32), ("dims", ctypes.c_int32 * 4)]
+
+
+class ams_attn(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -122,6 +128,15 @@ def load() -> ctypes.CDLL:
     lib.ams_lookup_workspace.argtypes = [i64, i32]
     lib.ams_lookup_bwd.restype = ctypes.c_int
     lib.ams_lookup_bwd.argtypes = [i32, i32, f, i32, i64, P, P, P, P, P, i32, P, i64, P, P, sz, P]
+    A = ctypes.POINTER(ams_attn)
+    rows = [P, i64]                                    # an array and its row stride
+    lists = [A, i32, P, i64, P, i64]                   # shape, samples, query and key offsets with their totals
+    lib.ams_xattn_workspace.restype = sz
+    lib.ams_xattn_workspace.argtypes = [A, i32, i64, i64]
+    lib.ams_xattn_fwd.restype = ctypes.c_int
+    lib.ams_xattn_fwd.argtypes = [*lists, *rows * 3, P, *rows, P, P, sz, P]
+    lib.ams_xattn_bwd.restype = ctypes.c_int
+    lib.ams_xattn_bwd.argtypes = [*lists, *rows * 3, P, *rows, P, *rows * 4, P, sz, P]
     for name, args in (("ams_peak_copy", [P, P, i64, i32, P]), ("ams_peak_read", [P, i64, i32, P, P]),
                        ("ams_peak_gather", [P, i64, i32, P, i32, i32, P, i32, P, P]),
                        ("ams_peak_mfma", [i32, P, i32, i32, P, P])):
@@ -441,6 +456,11 @@ class _Call:
             raise ValueError(f"{self.where}: {name} must be float32 or bfloat16, not {t.dtype}")
         return _STORAGE[t.dtype]
 
+    def storage_of(self, attn):
+        if attn.dtype not in (AMS_F32, AMS_BF16):
+            raise AmsError(3, self.where)
+        return torch.float32 if attn.dtype == AMS_F32 else torch.bfloat16
+
     def run(self, f, *args, stream=None):
         if stream is None:
             stream = torch.cuda.current_stream(self.device)
@@ -485,6 +505,56 @@ def ams_lookup_bwd(uniq, inv, occ_perm, uniq_off, n_uniq, n_uniq_cap: int, dout,
     wp = c.vec("ws", ws, torch.uint8, 0)
     c.run(load().ams_lookup_bwd, dt, D, float(scale), int(pad_id), n, *args, int(n_uniq_cap), dp, ldd, gp, wp,
           ws.numel(), stream=stream)
+
+
+def make_attn(n_heads: int, n_kv_heads: int, head_dim: int, dtype: str = "bf16", scale: float | None = None) -> ams_attn:
+    """ams_attn of these heads; scale: head_dim ** -0.5 unless given."""
+    return ams_attn({"f32": AMS_F32, "bf16": AMS_BF16}[dtype], int(n_heads), int(n_kv_heads), int(head_dim),
+                    float(head_dim) ** -0.5 if scale is None else float(scale))
+
+
+def ams_xattn_workspace(attn: ams_attn, B: int, n_q: int, n_k: int) -> int:
+    return load().ams_xattn_workspace(ctypes.byref(attn), int(B), int(n_q), int(n_k))
+
+
+def _xattn_inputs(c, attn, q_off, k_off, q, k, v, key_mask):
+    """(samples and offsets, the q / k / v arrays and mask) of a call, checked."""
+    B, n_q, n_k, i32 = q_off.numel() - 1, q.shape[0], k.shape[0], torch.int32
+    T = c.storage_of(attn)
+    if v.shape[0] != n_k:
+        raise ValueError(f"{c.where}: k and v have {n_k} and {v.shape[0]} rows")
+    hq, hk = (attn.n_heads, attn.head_dim), (attn.n_kv_heads, attn.head_dim)
+    lists = [ctypes.byref(attn), B, c.vec("q_off", q_off, i32, 1), n_q, c.vec("k_off", k_off, i32, B + 1), n_k]
+    arrays = [*c.rows("q", q, T, n_q, hq), *c.rows("k", k, T, n_k, hk), *c.rows("v", v, T, n_k, hk),
+              None if key_mask is None else c.vec("key_mask", key_mask, torch.uint8, n_k)]
+    return lists, arrays
+
+
+def ams_xattn_fwd(attn: ams_attn, q_off, k_off, q, k, v, out, lse, ws, key_mask=None, stream=None):
+    """Attention of each sample's queries q [n_q, heads, dim] to its keys k, v
+    [n_k, kv_heads, dim]; lse [n_q, heads] (None: not stored)."""
+    c = _Call("ams_xattn_fwd")
+    lists, arrays = _xattn_inputs(c, attn, q_off, k_off, q, k, v, key_mask)
+    n_q, T = q.shape[0], q.dtype
+    o = c.rows("out", out, T, n_q, (attn.n_heads, attn.head_dim))
+    lp = None if lse is None else c.vec("lse", lse, torch.float32, n_q * attn.n_heads)
+    wp = c.vec("ws", ws, torch.uint8, 0)
+    c.run(load().ams_xattn_fwd, *lists, *arrays, *o, lp, wp, ws.numel(), stream=stream)
+
+
+def ams_xattn_bwd(attn: ams_attn, q_off, k_off, q, k, v, out, lse, dout, dq, dk, dv, ws, key_mask=None, stream=None):
+    """Gradients dq, dk, dv (overwritten) of ams_xattn_fwd's inputs, from its
+    out and lse and the upstream gradient dout."""
+    c = _Call("ams_xattn_bwd")
+    lists, arrays = _xattn_inputs(c, attn, q_off, k_off, q, k, v, key_mask)
+    n_q, n_k, T = q.shape[0], k.shape[0], q.dtype
+    hq, hk = (attn.n_heads, attn.head_dim), (attn.n_kv_heads, attn.head_dim)
+    o = c.rows("out", out, T, n_q, hq)
+    lp = c.vec("lse", lse, torch.float32, n_q * attn.n_heads)
+    grads = [*c.rows("dout", dout, T, n_q, hq), *c.rows("dq", dq, T, n_q, hq), *c.rows("dk", dk, T, n_k, hk),
+             *c.rows("dv", dv, T, n_k, hk)]
+    wp = c.vec("ws", ws, torch.uint8, 0)
+    c.run(load().ams_xattn_bwd, *lists, *arrays, *o, lp, *grads, wp, ws.numel(), stream=stream)
 
 
 # ---------------------------------------------------------------- probes
