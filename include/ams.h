@@ -584,6 +584,55 @@ ams_status ams_xattn_bwd(const ams_attn *attn, int32_t B, const int32_t *q_off, 
                          const void *dout, int64_t ld_dout, void *dq, int64_t ld_dq, void *dk, int64_t ld_dk,
                          void *dv, int64_t ld_dv, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------ 8-bit cache ----
+ * The serving form: a user's keys and values kept between requests in pages of
+ * 8-bit codes.  A page holds `page` consecutive tokens of one sample; page p of
+ * the pool and key head h own `page` rows of head_dim codes,
+ *   codes[((p * n_kv_heads + h) * page + t) * head_dim + d],
+ * OCP e4m3 bytes, and one float scale[p * n_kv_heads + h], a power of two: the
+ * entry is code * scale.  k and v have arrays of their own.  Token t of sample i
+ * is token t % page of page page_table[i * max_pages + t / page]. */
+typedef struct {
+    int32_t n_kv_heads;  /* 1..4096 */
+    int32_t head_dim;    /* 1..128 */
+    int32_t page;        /* tokens of a page: 16, 32, 64 or 128 */
+    int32_t max_pages;   /* pages of a sample: columns of the page table (max_pages * page < 2^31) */
+    int64_t n_pages;     /* pages of the pool */
+} ams_cache;
+
+/* write: appends each sample's new tokens behind its start[i] tokens.
+ *       new_off [B+1] CSR offsets of the new tokens (device), rows k, v [n_new x
+ *       n_kv_heads x head_dim] in dtype (AMS_F32 or AMS_BF16) with row strides
+ *       ld_k, ld_v; start [B], page_table [B x max_pages] (device).
+ *       A touched page and head gets the least scale 2^e, e >= -100, with 448 *
+ *       scale >= the largest finite magnitude of its new tokens, or keeps the
+ *       scale that its earlier tokens have if that is larger; where the scale
+ *       grows the earlier codes are rounded to it.  Codes are entry / scale
+ *       rounded to nearest, ties to even, infinities to +-448, NaN to NaN.
+ *       Slots behind the last token are left as they were; a page that starts
+ *       with this write takes nothing from what it held.  The pages that one
+ *       call writes must be distinct.
+ *       Tokens with nowhere to go (start[i] < 0, past max_pages, a page outside
+ *       [0, n_pages)) are not written, and *dev_status (device, may be NULL)
+ *       becomes AMS_ERR_ID_RANGE; it is never cleared here.
+ * attn: ams_xattn_fwd of q [n_q x n_heads x head_dim] (attn->dtype) over the first
+ *       lengths[i] tokens of sample i's pages (at most max_pages * page of them;
+ *       several samples may share pages).  Tokens of a page outside [0, n_pages)
+ *       take no part.  attn and cache agree in n_kv_heads and head_dim (else
+ *       DIMS).  Codes enter the products exactly.  lse may be NULL.
+ *       ws: at least ams_cache_workspace(attn, cache, B, n_q) bytes.
+ * Host errors: NULL, DTYPE, DIMS (heads, head_dim, page), SIZE (as for
+ * ams_xattn_fwd; n_new, max_pages or n_pages out of range), WORKSPACE. */
+ams_status ams_cache_write(const ams_cache *cache, int32_t dtype, int32_t B, const int32_t *new_off, int64_t n_new,
+                           const int32_t *start, const int32_t *page_table, const void *k, int64_t ld_k,
+                           const void *v, int64_t ld_v, uint8_t *k_codes, float *k_scale, uint8_t *v_codes,
+                           float *v_scale, int32_t *dev_status, void *stream);
+size_t ams_cache_workspace(const ams_attn *attn, const ams_cache *cache, int32_t B, int64_t n_q);
+ams_status ams_cache_attn(const ams_attn *attn, const ams_cache *cache, int32_t B, const int32_t *q_off, int64_t n_q,
+                          const int32_t *lengths, const int32_t *page_table, const void *q, int64_t ld_q,
+                          const uint8_t *k_codes, const float *k_scale, const uint8_t *v_codes, const float *v_scale,
+                          void *out, int64_t ld_out, float *lse, void *ws, size_t ws_bytes, void *stream);
+
 /* ============================================================= probes ====
  * Achievable-peak probes of the device (they compute nothing of the method):
  * the rates the part delivers for plain HBM streams, for gathering table

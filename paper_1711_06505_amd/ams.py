@@ -29,7 +29,8 @@ EXPORTS = ["ams_status_str", "ams_build_info", "ams_dedup_workspace", "ams_dedup
            "ams_adagrad_rows", "ams_pool_query_fwd", "ams_pool_query_bwd",
            "ams_adam_update", "ams_pool_concat_fwd", "ams_pool_concat_bwd", "ams_dssm_workspace",
            "ams_dssm_fwd_bwd", "ams_lookup_fwd", "ams_lookup_workspace", "ams_lookup_bwd",
-           "ams_xattn_workspace", "ams_xattn_fwd", "ams_xattn_bwd", "ams_peak_copy", "ams_peak_read", "ams_peak_gather", "ams_peak_mfma"]
+           "ams_xattn_workspace", "ams_xattn_fwd", "ams_xattn_bwd", "ams_cache_write",
+           "ams_cache_workspace", "ams_cache_attn", "ams_peak_copy", "ams_peak_read", "ams_peak_gather", "ams_peak_mfma"]
 
 
 class AmsError(RuntimeError):
@@ -54,6 +55,11 @@ class ams_ctr(ctypes.Structure):
 class ams_attn(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class ams_cache(ctypes.Structure):
+    _fields_ = [("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int64)]
 
 
 _lib = None
@@ -137,6 +143,13 @@ def load() -> ctypes.CDLL:
     lib.ams_xattn_fwd.argtypes = [*lists, *rows * 3, P, *rows, P, P, sz, P]
     lib.ams_xattn_bwd.restype = ctypes.c_int
     lib.ams_xattn_bwd.argtypes = [*lists, *rows * 3, P, *rows, P, *rows * 4, P, sz, P]
+    K = ctypes.POINTER(ams_cache)
+    lib.ams_cache_write.restype = ctypes.c_int
+    lib.ams_cache_write.argtypes = [K, i32, i32, P, i64, P, P, *rows * 2, P, P, P, P, P, P]
+    lib.ams_cache_workspace.restype = sz
+    lib.ams_cache_workspace.argtypes = [A, K, i32, i64]
+    lib.ams_cache_attn.restype = ctypes.c_int
+    lib.ams_cache_attn.argtypes = [A, K, i32, P, i64, P, P, *rows, P, P, P, P, *rows, P, P, sz, P]
     for name, args in (("ams_peak_copy", [P, P, i64, i32, P]), ("ams_peak_read", [P, i64, i32, P, P]),
                        ("ams_peak_gather", [P, i64, i32, P, i32, i32, P, i32, P, P]),
                        ("ams_peak_mfma", [i32, P, i32, i32, P, P])):
@@ -555,6 +568,59 @@ def ams_xattn_bwd(attn: ams_attn, q_off, k_off, q, k, v, out, lse, dout, dq, dk,
              *c.rows("dv", dv, T, n_k, hk)]
     wp = c.vec("ws", ws, torch.uint8, 0)
     c.run(load().ams_xattn_bwd, *lists, *arrays, *o, lp, *grads, wp, ws.numel(), stream=stream)
+
+
+def make_cache(n_kv_heads: int, head_dim: int, page: int, max_pages: int, n_pages: int) -> ams_cache:
+    """ams_cache: pages of `page` tokens, max_pages of them per sample, n_pages in the pool."""
+    return ams_cache(int(n_kv_heads), int(head_dim), int(page), int(max_pages), int(n_pages))
+
+
+def _cache_arrays(c, cache, B, page_table, k_codes, k_scale, v_codes, v_scale):
+    heads = cache.n_pages * cache.n_kv_heads
+    codes = heads * cache.page * cache.head_dim
+    return (c.vec("page_table", page_table, torch.int32, B * cache.max_pages),
+            [c.vec("k_codes", k_codes, torch.uint8, codes), c.vec("k_scale", k_scale, torch.float32, heads),
+             c.vec("v_codes", v_codes, torch.uint8, codes), c.vec("v_scale", v_scale, torch.float32, heads)])
+
+
+def ams_cache_write(cache: ams_cache, new_off, start, page_table, k, v, k_codes, k_scale, v_codes, v_scale,
+                    dev_status=None, stream=None):
+    """Appends new tokens' keys and values k, v [n_new, kv_heads, dim] behind
+    each sample's start[i] tokens; codes [n_pages, kv_heads, page, dim] uint8
+    and scales [n_pages, kv_heads]."""
+    c = _Call("ams_cache_write")
+    B, n, i32 = new_off.numel() - 1, k.shape[0], torch.int32
+    inner = (cache.n_kv_heads, cache.head_dim)
+    dt = c.storage("k", k)
+    if v.shape[0] != n:
+        raise ValueError(f"{c.where}: k and v have {n} and {v.shape[0]} rows")
+    rows = [*c.rows("k", k, k.dtype, n, inner), *c.rows("v", v, k.dtype, n, inner)]
+    op, sp = c.vec("new_off", new_off, i32, 1), c.vec("start", start, i32, B)
+    tp, arrays = _cache_arrays(c, cache, B, page_table, k_codes, k_scale, v_codes, v_scale)
+    st = None if dev_status is None else c.vec("dev_status", dev_status, i32, 1)
+    c.run(load().ams_cache_write, ctypes.byref(cache), dt, B, op, n, sp, tp, *rows, *arrays, st, stream=stream)
+
+
+def ams_cache_workspace(attn: ams_attn, cache: ams_cache, B: int, n_q: int) -> int:
+    return load().ams_cache_workspace(ctypes.byref(attn), ctypes.byref(cache), int(B), int(n_q))
+
+
+def ams_cache_attn(attn: ams_attn, cache: ams_cache, q_off, lengths, page_table, q, k_codes, k_scale, v_codes, v_scale,
+                   out, ws, lse=None, stream=None):
+    """Attention of each sample's queries q [n_q, heads, dim] to the first
+    lengths[i] tokens that its pages hold."""
+    c = _Call("ams_cache_attn")
+    B, n_q, i32, T = q_off.numel() - 1, q.shape[0], torch.int32, c.storage_of(attn)
+    if (attn.n_kv_heads, attn.head_dim) != (cache.n_kv_heads, cache.head_dim):
+        raise AmsError(4, c.where)
+    hq = (attn.n_heads, attn.head_dim)
+    qp, op = c.rows("q", q, T, n_q, hq), c.rows("out", out, T, n_q, hq)
+    fp, lp = c.vec("q_off", q_off, i32, 1), c.vec("lengths", lengths, i32, B)
+    tp, arrays = _cache_arrays(c, cache, B, page_table, k_codes, k_scale, v_codes, v_scale)
+    ep = None if lse is None else c.vec("lse", lse, torch.float32, n_q * attn.n_heads)
+    wp = c.vec("ws", ws, torch.uint8, 0)
+    c.run(load().ams_cache_attn, ctypes.byref(attn), ctypes.byref(cache), B, fp, n_q, lp, tp, *qp, *arrays, *op, ep, wp,
+          ws.numel(), stream=stream)
 
 
 # ---------------------------------------------------------------- probes

@@ -258,9 +258,10 @@ struct AttnArgs {
     int64_t ld_dq, ld_dk, ld_dv;
 };
 
-// Last sample i whose first tile, floor(off[i] mul / tile) + i, is at most
+// Last sample i whose first tile, floor(off[i] mul / tile) + own i, is at most
 // `at`, by a search of 64 probes at a time.
-__device__ __forceinline__ int find_sample(const int32_t *off, int B, int64_t n, int mul, int tile_shift, int64_t at)
+__device__ __forceinline__ int find_sample(const int32_t *off, int B, int64_t n, int mul, int tile_shift, int own,
+                                           int64_t at)
 {
     const int lane = ams_lane();
     int lo = 0, len = B;
@@ -271,7 +272,7 @@ __device__ __forceinline__ int find_sample(const int32_t *off, int B, int64_t n,
         if (lane * step < len) {
             int64_t o = off[i];
             o = o < 0 ? 0 : (o > n ? n : o);
-            le = ((o * mul) >> tile_shift) + i <= at;
+            le = ((o * mul) >> tile_shift) + (int64_t)own * i <= at;
         }
         int c = __popcll(ams_ballot(le));
         c = c < 1 ? 1 : c;
@@ -292,7 +293,7 @@ struct Span {
 __device__ __forceinline__ Span span_of(const int32_t *off, int B, int64_t n, int mul, int tile_shift, int64_t at)
 {
     Span s;
-    s.i = find_sample(off, B, n, mul, tile_shift, at);
+    s.i = find_sample(off, B, n, mul, tile_shift, 1, at);
     s.begin = clamp_off(off[s.i], n);
     const int end = clamp_off(off[s.i + 1], n);
     s.count = end > s.begin ? end - s.begin : 0;
