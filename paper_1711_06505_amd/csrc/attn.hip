@@ -18,7 +18,7 @@ namespace {
 template <class T, int DH, int PB>
 __global__ __launch_bounds__(kAttnThreads) void attn_dq_k(AttnArgs a)
 {
-    constexpr int SF = Num<T>::SF, NF = DH / (4 * Num<T>::EP), VD = DH / 16;
+    constexpr int NF = DH / (4 * Num<T>::EP), VD = DH / 16;
     __shared__ float s_o[kAttnWaves][kRowTile][DH + 4];
     const int lane = ams_lane(), m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);
@@ -97,9 +97,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dq_k(AttnArgs a)
                 ds[j] = live[j] ? p * (dp[r] - delta) * a.scale : 0.f;
             }
         }
-        Frag sf[SF];                                   // bf16: dS rounded once, as P is in the forward
-        pack_stream<T>(ds, sf);
-        mma_slice<T, DH>(acc, kk, sf);
+        mma_slice<T, DH>(acc, kk, Stream<T>(ds));
     }
     float o[4 * VD];
     acc_in_order<VD>(acc, 1.f, o);
@@ -129,7 +127,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dq_k(AttnArgs a)
 template <class T, int DH, int PB>
 __global__ __launch_bounds__(kAttnThreads) void attn_dkv_k(AttnArgs a)
 {
-    constexpr int SF = Num<T>::SF, NF = DH / (4 * Num<T>::EP), VD = DH / 16;
+    constexpr int NF = DH / (4 * Num<T>::EP), VD = DH / 16;
     const int lane = ams_lane(), m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);
     int64_t b = blockIdx.x;
@@ -207,11 +205,8 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dkv_k(AttnArgs a)
                     os.zero(j);
                 }
         }
-        Frag pf[SF], sf[SF];
-        pack_stream<T>(p, pf);
-        pack_stream<T>(ds, sf);
-        mma_slice<T, DH>(av, os, pf);
-        mma_slice<T, DH>(ak, qs, sf);
+        mma_slice<T, DH>(av, os, Stream<T>(p));
+        mma_slice<T, DH>(ak, qs, Stream<T>(ds));
     }
     if (!mine) return;
     float o[4 * VD];

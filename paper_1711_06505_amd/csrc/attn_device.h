@@ -177,28 +177,40 @@ template <class T, int DH> struct Slice {
     }
 };
 
-// Probabilities (or their gradients) of the lane's 8 streamed entries as operand.
-template <class T> __device__ __forceinline__ void pack_stream(const float *p, Frag *f)
-{
-    if constexpr (sizeof(T) == 4) {
+// Probabilities (or their gradients) of the lane's 8 streamed entries as
+// operand.  bf16 takes each as a pair, its rounding and the rounded rest, so
+// that it enters within 2^-17 of its float32 value: the second instruction
+// costs nothing where these kernels run, which is bound by memory, and a
+// rounding to 8 bits here would be as large an error as the output's own.
+template <class T> struct Stream {
+    Frag f[2];
+    __device__ __forceinline__ explicit Stream(const float *p)
+    {
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j >> 2].f[j & 3] = p[j];
-    } else {
+            for (int j = 0; j < 8; ++j) f[j >> 2].f[j & 3] = p[j];
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[0].u[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t h = pack_bf16(p[2 * i], p[2 * i + 1]);
+                f[0].u[i] = h;
+                f[1].u[i] = pack_bf16(p[2 * i] - __uint_as_float(h << 16),
+                                      p[2 * i + 1] - __uint_as_float(h & 0xffff0000u));
+            }
+        }
     }
-}
+};
 
-// acc[t] += slice tile t times the packed stream, over all VD tiles.
+// acc[t] += slice tile t times the stream, over all VD tiles.
 template <class T, int DH>
-__device__ __forceinline__ void mma_slice(f32x4 *acc, const Slice<T, DH> &s, const Frag *p)
+__device__ __forceinline__ void mma_slice(f32x4 *acc, const Slice<T, DH> &s, const Stream<T> &p)
 {
 #pragma unroll
     for (int t = 0; t < Slice<T, DH>::VD; ++t) {
         Frag f[Num<T>::SF];
         s.frags(t, f);
 #pragma unroll
-        for (int i = 0; i < Num<T>::SF; ++i) acc[t] = mma<T>(f[i], p[i], acc[t]);
+        for (int i = 0; i < 2; ++i) acc[t] = mma<T>(f[sizeof(T) == 4 ? i : 0], p.f[i], acc[t]);
     }
 }
 
@@ -341,7 +353,7 @@ template <class T> __device__ __forceinline__ void decode4(uint32_t w, uint32_t 
 template <class T, int DH, int PB, bool PAGED>
 __global__ __launch_bounds__(kAttnThreads) void attn_fwd_k(AttnArgs a)
 {
-    constexpr int EP = Num<T>::EP, SF = Num<T>::SF, NF = DH / (4 * EP), VD = DH / 16;
+    constexpr int EP = Num<T>::EP, NF = DH / (4 * EP), VD = DH / 16;
     constexpr int CB = PB / (int)sizeof(T);           // codes of a piece: as many as elements
     constexpr int kPad = DH + 4;
     __shared__ float s_o[kAttnWaves][kRowTile][kPad];
@@ -479,9 +491,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_fwd_k(AttnArgs a)
 #pragma unroll
             for (int j = 0; j < 8; ++j) p[j] = live[j] ? p[j] * sv[j >> 2] : 0.f;      // a power of two: exact
         }
-        Frag pf[SF];                                  // bf16: probabilities rounded once, their sum l is not
-        pack_stream<T>(p, pf);
-        mma_slice<T, DH>(acc, vv, pf);
+        mma_slice<T, DH>(acc, vv, Stream<T>(p));
     }
 
     // join the four waves
