@@ -571,7 +571,8 @@ typedef struct {
  *       bf16 of the weights (of their gradients) before the second product.
  * ws:   at least ams_xattn_workspace(attn, B, n_q, n_k) bytes, for either call.
  * Host errors: NULL, DTYPE, DIMS (heads, head_dim), SIZE (a negative size,
- * n_q * n_heads / n_kv_heads or n_k above 2^31 - 1, a stride below the width,
+ * n_q * n_heads / n_kv_heads or n_k above 2^31 - 1, a stride below the width
+ * or above 2^24,
  * more than 2^24 - 1 tiles of 16 rows or 64 keys in all), WORKSPACE. */
 size_t ams_xattn_workspace(const ams_attn *attn, int32_t B, int64_t n_q, int64_t n_k);
 ams_status ams_xattn_fwd(const ams_attn *attn, int32_t B, const int32_t *q_off, int64_t n_q, const int32_t *k_off,

@@ -9,182 +9,259 @@
 // stream keys as the forward does; dK's and dV's own keys, 16 a wave, and
 // stream the rows (all heads of the group), so both their contractions have
 // the operand layouts of the forward with rows and keys exchanged.
+#include <initializer_list>
+
 #include "attn_device.h"
 
 namespace {
 
-// -------------------------------------------------------------- dQ, delta
-
-template <class T, int DH, int PB>
-__global__ __launch_bounds__(kAttnThreads) void attn_dq_k(AttnArgs a)
+// delta = <dO, O> of the lane's row (pieces of it in each lane group).
+template <class T, int NF> __device__ __forceinline__ float row_delta(const Frag *df, const Frag *of)
 {
-    constexpr int NF = DH / (4 * Num<T>::EP), VD = DH / 16;
-    __shared__ float s_o[kAttnWaves][kRowTile][DH + 4];
-    const int lane = ams_lane(), m = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);
-    int64_t b = blockIdx.x;
-    const int split = (int)(b % a.nsplit);
-    b /= a.nsplit;
-    const int h = (int)(b % a.Hk);
-    const Span rows = span_of(a.q_off, a.B, a.n_q, a.G, 4, b / a.Hk);
-    const int64_t R = (int64_t)rows.count * a.G;
-    if (rows.first < 0 || rows.first >= R) return;
-    const int64_t r_mine = rows.first + m;
-    const Row row = row_at(a, rows.begin, h, (int)(r_mine < R ? r_mine : R - 1));
-    const int k0 = clamp_off(a.k_off[rows.i], a.n_k), k1 = clamp_off(a.k_off[rows.i + 1], a.n_k);
-    int lo, hi;
-    split_range(k1 > k0 ? k1 - k0 : 0, split, a.nsplit, lo, hi);
-
-    Frag qf[NF], df[NF], of[NF];
-    load_row<T, DH, PB>(qf, (const T *)a.q + row.query * a.ld_q + (int64_t)row.head * a.D, g, a.D);
-    load_row<T, DH, PB>(df, (const T *)a.dout + row.query * a.ld_dout + (int64_t)row.head * a.D, g, a.D);
-    load_row<T, DH, PB>(of, (const T *)a.o + row.query * a.ld_o + (int64_t)row.head * a.D, g, a.D);
-    const int64_t at = row.query * a.H + row.head;
-    const float lse = a.lse[at];
-    const bool live_row = lse != kNegInf;             // a row without keys: its upstream gradient goes nowhere
-    float delta = 0.f;
+    float d = 0.f;
 #pragma unroll
     for (int f = 0; f < NF; ++f)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (sizeof(T) == 4) {
-                delta += df[f].f[i] * of[f].f[i];
+                d += df[f].f[i] * of[f].f[i];
             } else {
-                delta += __uint_as_float(df[f].u[i] << 16) * __uint_as_float(of[f].u[i] << 16);
-                delta += __uint_as_float(df[f].u[i] & 0xffff0000u) * __uint_as_float(of[f].u[i] & 0xffff0000u);
+                d += __uint_as_float(df[f].u[i] << 16) * __uint_as_float(of[f].u[i] << 16);
+                d += __uint_as_float(df[f].u[i] & 0xffff0000u) * __uint_as_float(of[f].u[i] & 0xffff0000u);
             }
         }
-    delta = live_row ? sum_groups(delta) : 0.f;
-    if (split == 0 && wave == 0 && g == 0 && r_mine < R) a.delta[at] = delta;
+    return sum_groups(d);
+}
 
-    const float c = a.scale * kLog2e, lse2 = live_row ? lse * kLog2e : 0.f;
-    f32x4 acc[VD];
+// -------------------------------------------------------------- dQ, delta
+
+// Tiles, waves and splits as the forward's.
+template <class T, int DH, int PB, int RT, int WK>
+__device__ __forceinline__ void dq_tile(const AttnArgs &a, int64_t block,
+                                        float (*s_o)[WK > 1 ? kRowTile * RT : 1][DH + 4])
+{
+    constexpr int NF = DH / (4 * Num<T>::EP), VD = DH / 16, ES = (int)sizeof(T);
+    constexpr int kRows = kRowTile * RT, kTileShift = RT == 2 ? 5 : 4;
+    const int lane = ams_lane(), m = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);
+    const Work wk = work_of(WK == 1 ? block * kAttnWaves + wave : block, a);
+    const int h = wk.h;
+    if (wk.tile >= a.tiles) return;
+    const Span rows = span_of(a.q_off, a.B, a.n_q, a.G, kTileShift, wk.tile);
+    const int64_t R = (int64_t)rows.count * a.G;
+    if (rows.first < 0 || rows.first >= R || R <= a.few_rows) return;
+    const int k0 = clamp_off(a.k_off[rows.i], a.n_k), k1 = clamp_off(a.k_off[rows.i + 1], a.n_k);
+    int lo, hi;
+    split_range(k1 > k0 ? k1 - k0 : 0, wk.split, a.nsplit, lo, hi);
+
+    const RowCols<T, DH, PB> rc(g, a.D);
+    Frag qf[RT][NF], df[RT][NF];
+    Row row[RT];
+    float lse2[RT], delta[RT];
+    bool on[RT];                                      // a row without keys: its upstream gradient goes nowhere
+    const float c = a.scale * kLog2e;
+    f32x4 acc[RT][VD];
 #pragma unroll
-    for (int t = 0; t < VD; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const T *kp = (const T *)a.k + (int64_t)h * a.D, *vp = (const T *)a.v + (int64_t)h * a.D;
-    for (int kb = lo + wave * kKeyTile; kb < hi; kb += kAttnWaves * kKeyTile) {
+    for (int t = 0; t < RT; ++t) {
+        const int64_t r = rows.first + 16 * t + m;
+        row[t] = row_at(a, rows.begin, h, (int)(r < R ? r : R - 1));
+        const int64_t col = (int64_t)row[t].head * a.D;
+        Frag of[NF];
+        rc.load(qf[t], (const char *)a.q + (row[t].query * a.ld_q + col) * ES, 0);
+        rc.load(df[t], (const char *)a.dout + (row[t].query * a.ld_dout + col) * ES, 0);
+        rc.load(of, (const char *)a.o + (row[t].query * a.ld_o + col) * ES, 0);
+        rc.clean(qf[t]);
+        rc.clean(df[t]);
+        rc.clean(of);
+        const int64_t at = row[t].query * a.H + row[t].head;
+        const float lse = a.lse[at];
+        on[t] = lse != kNegInf;
+        lse2[t] = on[t] ? lse * kLog2e : 0.f;
+        delta[t] = row_delta<T, NF>(df[t], of);
+        delta[t] = on[t] ? delta[t] : 0.f;
+        if (wk.split == 0 && (WK == 1 || wave == 0) && g == 0 && r < R) a.delta[at] = delta[t];
+#pragma unroll
+        for (int i = 0; i < VD; ++i) acc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const uint32_t ldk = (uint32_t)(a.ld_k * ES), ldv = (uint32_t)(a.ld_v * ES);
+    uint32_t krow[2] = {m * ldk, (16 + m) * ldk}, vrow[2] = {m * ldv, (16 + m) * ldv}, srow[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) srow[j] = (uint32_t)stream_of(j, g) * ldk;
+    const Cols<T, VD, PB> scol(m * VD, a.D);
+
+    for (int kb = lo + (WK == 1 ? 0 : wave * kKeyTile); kb < hi; kb += WK * kKeyTile) {
+        Frag kf[2][NF], vf[2][NF];
         Slice<T, DH> kk;
-        bool live[8];
+        const uint32_t live = live_bits(k0 + kb, k0 + hi, a.mask);
+        if (kb + kKeyTile > hi) {
+            const int last = hi - 1 - kb;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            int key = kb + stream_of(j, g);
-            live[j] = key < hi && live_row;
-            key = k0 + (key < hi ? key : hi - 1);
-            load_elems<T, VD, PB>(kk.w[j], kp + (int64_t)key * a.ld_k, m * VD, a.D);
-            if (a.mask && a.mask[key] == 0) {
-                live[j] = false;
-                kk.zero(j);
+            for (int t = 0; t < 2; ++t) {
+                krow[t] = (uint32_t)min(16 * t + m, last) * ldk;
+                vrow[t] = (uint32_t)min(16 * t + m, last) * ldv;
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) srow[j] = (uint32_t)min(stream_of(j, g), last) * ldk;
         }
-        float ds[8];
+        const char *kp = (const char *)a.k + ((int64_t)(k0 + kb) * a.ld_k + (int64_t)h * a.D) * ES;
+        const char *vp = (const char *)a.v + ((int64_t)(k0 + kb) * a.ld_v + (int64_t)h * a.D) * ES;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            Frag kf[NF], vf[NF];
-            int key = kb + 16 * t + m;
-            key = k0 + (key < hi ? key : hi - 1);
-            load_row<T, DH, PB>(kf, kp + (int64_t)key * a.ld_k, g, a.D);
-            load_row<T, DH, PB>(vf, vp + (int64_t)key * a.ld_v, g, a.D);
-            f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f}, dp = s;
-#pragma unroll
-            for (int f = 0; f < NF; ++f) {
-                s = mma<T>(kf[f], qf[f], s);
-                dp = mma<T>(vf[f], df[f], dp);
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int j = 4 * t + r;
-                const float p = __builtin_amdgcn_exp2f(s[r] * c - lse2);
-                ds[j] = live[j] ? p * (dp[r] - delta) * a.scale : 0.f;
-            }
+            rc.load(kf[t], kp, krow[t]);
+            rc.load(vf[t], vp, vrow[t]);
         }
-        mma_slice<T, DH>(acc, kk, Stream<T>(ds));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) scol.load(kk.w[j], kp, srow[j]);
+        if (live != 0xffffffffu) kk.keep(live, g);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float ds[8];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f}, dp = s;
+#pragma unroll
+                for (int f = 0; f < NF; ++f) {
+                    s = mma<T>(kf[t][f], qf[rt][f], s);
+                    dp = mma<T>(vf[t][f], df[rt][f], dp);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(s[r] * c - lse2[rt]);
+                    ds[4 * t + r] = on[rt] ? p * (dp[r] - delta[rt]) * a.scale : 0.f;
+                }
+            }
+            if (live != 0xffffffffu) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) ds[j] = (live >> (4 * g + stream_of(j, 0)) & 1) ? ds[j] : 0.f;
+            }
+            mma_slice<T, DH>(acc[rt], kk, Stream<T>(ds));
+        }
     }
-    float o[4 * VD];
-    acc_in_order<VD>(acc, 1.f, o);
+    if constexpr (WK == 1) {
 #pragma unroll
-    for (int i = 0; i < 4 * VD; ++i) s_o[wave][m][4 * g * VD + i] = o[i];
-    __syncthreads();
-    const int r = threadIdx.x / 16, d = (threadIdx.x % 16) * VD;
-    const int64_t ro = rows.first + r;
-    if (ro >= R) return;
-    float y[VD];
-#pragma unroll
-    for (int e = 0; e < VD; ++e) y[e] = (s_o[0][r][d + e] + s_o[1][r][d + e]) + (s_o[2][r][d + e] + s_o[3][r][d + e]);
-    const Row ow = row_at(a, rows.begin, h, (int)ro);
-    if (a.nsplit > 1) {
-        float *p = a.part_o + ((int64_t)split * a.n_q * a.H + ow.query * a.H + ow.head) * a.D;
-#pragma unroll
-        for (int e = 0; e < VD; ++e)
-            if (d + e < a.D) p[d + e] = y[e];
+        for (int t = 0; t < RT; ++t) {
+            if (rows.first + 16 * t + m >= R) continue;
+            float o[4 * VD];
+            acc_in_order<VD>(acc[t], 1.f, o);
+            store_elems<T, 4 * VD, PB>((T *)a.dq + row[t].query * a.ld_dq + (int64_t)row[t].head * a.D, 4 * g * VD,
+                                       a.D, o);
+        }
         return;
     }
-    store_elems<T, VD, PB>((T *)a.dq + ow.query * a.ld_dq + (int64_t)ow.head * a.D, d, a.D, y);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        float o[4 * VD];
+        acc_in_order<VD>(acc[t], 1.f, o);
+#pragma unroll
+        for (int i = 0; i < 4 * VD; ++i) s_o[wave % WK][(16 * t + m) % (WK > 1 ? kRows : 1)][4 * g * VD + i] = o[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int r = 16 * t + threadIdx.x / 16, d = (threadIdx.x % 16) * VD, rr = r % (WK > 1 ? kRows : 1);
+        const int64_t ro = rows.first + r;
+        if (ro >= R) return;
+        float y[VD];
+#pragma unroll
+        for (int e = 0; e < VD; ++e)
+            y[e] = (s_o[0][rr][d + e] + s_o[1 % WK][rr][d + e]) + (s_o[2 % WK][rr][d + e] + s_o[3 % WK][rr][d + e]);
+        const Row ow = row_at(a, rows.begin, h, (int)ro);
+        if (a.nsplit > 1) {
+            float *p = a.part_o + ((int64_t)wk.split * a.n_q * a.H + ow.query * a.H + ow.head) * a.D;
+#pragma unroll
+            for (int e = 0; e < VD; ++e)
+                if (d + e < a.D) p[d + e] = y[e];
+            continue;
+        }
+        store_elems<T, VD, PB>((T *)a.dq + ow.query * a.ld_dq + (int64_t)ow.head * a.D, d, a.D, y);
+    }
+}
+
+// Where attn_bwd_few_k has the small samples, the grid is a fixed number of
+// blocks that first look whether there is any other (a.any_many).
+template <class T, int DH, int PB, int RT, int WK>
+__global__ __launch_bounds__(kAttnThreads, (waves_per_simd<T, DH, 2 * RT>())) void attn_dq_k(AttnArgs a)
+{
+    __shared__ float s_o[WK > 1 ? WK : 1][WK > 1 ? kRowTile * RT : 1][DH + 4];
+    if (a.few_rows >= 0 && *a.any_many == 0) return;
+    for (int64_t b = blockIdx.x; b < a.blocks; b += gridDim.x) {
+        dq_tile<T, DH, PB, RT, WK>(a, b, s_o);
+        __syncthreads();                               // s_o is free again
+    }
 }
 
 // ----------------------------------------------------------------- dK, dV
 
-// One block per (64 keys of a sample, key head, split of the rows).
-template <class T, int DH, int PB>
-__global__ __launch_bounds__(kAttnThreads) void attn_dkv_k(AttnArgs a)
+// One wave per (16 keys of a sample, key head, split of the rows), four
+// neighbouring key tiles to a block (they read the same rows).
+template <class T, int DH, int PB> __device__ __forceinline__ void dkv_tile(const AttnArgs &a, int64_t block)
 {
-    constexpr int NF = DH / (4 * Num<T>::EP), VD = DH / 16;
+    constexpr int NF = DH / (4 * Num<T>::EP), VD = DH / 16, ES = (int)sizeof(T);
     const int lane = ams_lane(), m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);
-    int64_t b = blockIdx.x;
-    const int split = (int)(b % a.nsplit);
-    b /= a.nsplit;
-    const int h = (int)(b % a.Hk);
-    const Span keys = span_of(a.k_off, a.B, a.n_k, 1, 6, b / a.Hk);
+    const Work wk = work_of(block, a);
+    const int h = wk.h;
+    const Span keys = span_of(a.k_off, a.B, a.n_k, 1, 6, wk.tile);
     const int64_t first = keys.first + wave * 16;
     if (keys.first < 0 || first >= keys.count) return;
     const int q0 = clamp_off(a.q_off[keys.i], a.n_q), q1 = clamp_off(a.q_off[keys.i + 1], a.n_q);
     const int64_t R = q1 > q0 ? (int64_t)(q1 - q0) * a.G : 0;
+    if (R <= a.few_rows) return;
     int lo, hi;
-    split_range((int)R, split, a.nsplit, lo, hi);
+    split_range((int)R, wk.split, a.nsplit, lo, hi);
 
     const bool mine = first + m < keys.count;
     const int64_t key = keys.begin + (mine ? first + m : keys.count - 1);
     const bool live_key = mine && !(a.mask && a.mask[key] == 0);
+    const RowCols<T, DH, PB> rc(g, a.D);
+    const Cols<T, VD, PB> scol(m * VD, a.D);
     Frag kf[NF], vf[NF];
-    load_row<T, DH, PB>(kf, (const T *)a.k + key * a.ld_k + (int64_t)h * a.D, g, a.D);
-    load_row<T, DH, PB>(vf, (const T *)a.v + key * a.ld_v + (int64_t)h * a.D, g, a.D);
+    rc.load(kf, (const char *)a.k + (key * a.ld_k + (int64_t)h * a.D) * ES, 0);
+    rc.load(vf, (const char *)a.v + (key * a.ld_v + (int64_t)h * a.D) * ES, 0);
+    rc.clean(kf);
+    rc.clean(vf);
     const float c = a.scale * kLog2e;
     f32x4 ak[VD], av[VD];
 #pragma unroll
     for (int t = 0; t < VD; ++t) ak[t] = av[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     for (int rb = lo; rb < hi; rb += kKeyTile) {
+        // the step's first query is the same in all lanes; a row lies at most 32 queries on
+        const int qb = __builtin_amdgcn_readfirstlane(a.by_g.div(rb));
+        const int64_t query = (int64_t)q0 + qb;
+        const char *qp = (const char *)a.q + (query * a.ld_q + (int64_t)h * a.G * a.D) * ES;
+        const char *dp_ = (const char *)a.dout + (query * a.ld_dout + (int64_t)h * a.G * a.D) * ES;
+        const float *lp = a.lse + query * a.H + h * a.G, *tp = a.delta + query * a.H + h * a.G;
         Slice<T, DH> qs, os;
+        Frag qf[2][NF], df[2][NF];
         float lse2[8], delta[8];
         bool live[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            int r = rb + stream_of(j, g);
-            live[j] = r < hi;
-            r = r < hi ? r : hi - 1;
-            const Row w = row_at(a, q0, h, r);
-            const int64_t at = w.query * a.H + w.head;
-            const float l = a.lse[at];
-            live[j] = live[j] && l != kNegInf;
+            const int r = rb + stream_of(j, g), rr = r < hi ? r : hi - 1, qq = a.by_g.div(rr), hh = rr - qq * a.G;
+            const uint32_t dq = (uint32_t)(qq - qb), col = (uint32_t)(hh * a.D * ES);
+            const float l = lp[dq * a.H + hh];
+            live[j] = r < hi && l != kNegInf;
             lse2[j] = l * kLog2e;
-            delta[j] = a.delta[at];
-            load_elems<T, VD, PB>(qs.w[j], (const T *)a.q + w.query * a.ld_q + (int64_t)w.head * a.D, m * VD, a.D);
-            load_elems<T, VD, PB>(os.w[j], (const T *)a.dout + w.query * a.ld_dout + (int64_t)w.head * a.D, m * VD,
-                                  a.D);
+            delta[j] = tp[dq * a.H + hh];
+            scol.load(qs.w[j], qp, dq * (uint32_t)(a.ld_q * ES) + col);
+            scol.load(os.w[j], dp_, dq * (uint32_t)(a.ld_dout * ES) + col);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int r = rb + 16 * t + m, rr = r < hi ? r : hi - 1, qq = a.by_g.div(rr), hh = rr - qq * a.G;
+            const uint32_t dq = (uint32_t)(qq - qb), col = (uint32_t)(hh * a.D * ES);
+            rc.load(qf[t], qp, dq * (uint32_t)(a.ld_q * ES) + col);
+            rc.load(df[t], dp_, dq * (uint32_t)(a.ld_dout * ES) + col);
         }
         float p[8], ds[8];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            Frag qf[NF], df[NF];
-            const int r = rb + 16 * t + m;
-            const Row w = row_at(a, q0, h, r < hi ? r : hi - 1);
-            load_row<T, DH, PB>(qf, (const T *)a.q + w.query * a.ld_q + (int64_t)w.head * a.D, g, a.D);
-            load_row<T, DH, PB>(df, (const T *)a.dout + w.query * a.ld_dout + (int64_t)w.head * a.D, g, a.D);
             f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f}, dp = s;
 #pragma unroll
             for (int f = 0; f < NF; ++f) {
-                s = mma<T>(qf[f], kf[f], s);
-                dp = mma<T>(df[f], vf[f], dp);
+                s = mma<T>(qf[t][f], kf[f], s);
+                dp = mma<T>(df[t][f], vf[f], dp);
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -211,7 +288,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dkv_k(AttnArgs a)
     if (!mine) return;
     float o[4 * VD];
     if (a.nsplit > 1) {
-        float *p = a.part_o + ((int64_t)split * a.n_k * a.Hk + key * a.Hk + h) * 2 * a.D;
+        float *p = a.part_o + ((int64_t)wk.split * a.n_k * a.Hk + key * a.Hk + h) * 2 * a.D;
         acc_in_order<VD>(ak, 1.f, o);
 #pragma unroll
         for (int i = 0; i < 4 * VD; ++i)
@@ -226,6 +303,231 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dkv_k(AttnArgs a)
     store_elems<T, 4 * VD, PB>((T *)a.dk + key * a.ld_dk + (int64_t)h * a.D, 4 * g * VD, a.D, o);
     acc_in_order<VD>(av, 1.f, o);
     store_elems<T, 4 * VD, PB>((T *)a.dv + key * a.ld_dv + (int64_t)h * a.D, 4 * g * VD, a.D, o);
+}
+
+template <class T, int DH, int PB>
+__global__ __launch_bounds__(kAttnThreads) void attn_dkv_k(AttnArgs a)
+{
+    if (a.few_rows >= 0 && *a.any_many == 0) return;
+    for (int64_t b = blockIdx.x; b < a.blocks; b += gridDim.x) dkv_tile<T, DH, PB>(a, b);
+}
+
+// ------------------------------------------- dQ, dK, dV of few rows at once
+
+// A sample whose rows fit one tile of 16 RT (a.few_rows; the others are left to
+// the two kernels above): one wave per (sample, key head, split of the keys)
+// keeps the rows in registers and reads each key once.  A key's scores are
+// formed twice from the same operands, once with a row per lane (for dQ, which
+// contracts over keys) and once with a key per lane (for dK and dV, which
+// contract over rows); a key tile's dK and dV are complete at once.  One more
+// block looks whether a sample has more rows than that.
+template <class T, int DH, int PB, int RT>
+__global__ __launch_bounds__(kAttnThreads, (waves_per_simd<T, DH, RT>())) void attn_bwd_few_k(AttnArgs a)
+{
+    if (blockIdx.x == gridDim.x - 1) {
+        bool found = false;
+#pragma unroll 4
+        for (int s = threadIdx.x; s < a.B; s += kAttnThreads)
+            found |= (int64_t)(clamp_off(a.q_off[s + 1], a.n_q) - clamp_off(a.q_off[s], a.n_q)) * a.G > a.few_rows;
+        const int any = __syncthreads_or(found);
+        if (threadIdx.x == 0) *a.any_many = any;
+        return;
+    }
+    constexpr int NF = DH / (4 * Num<T>::EP), VD = DH / 16, ES = (int)sizeof(T);
+    const int lane = ams_lane(), m = lane & 15, g = lane >> 4;
+    const Work wk = work_of((int64_t)blockIdx.x * kAttnWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE), a);
+    const int h = wk.h;
+    if (wk.tile >= a.B) return;
+    const int i = (int)wk.tile;
+    const int q0 = clamp_off(a.q_off[i], a.n_q), q1 = clamp_off(a.q_off[i + 1], a.n_q);
+    const int k0 = clamp_off(a.k_off[i], a.n_k), k1 = clamp_off(a.k_off[i + 1], a.n_k);
+    const int64_t R64 = q1 > q0 ? (int64_t)(q1 - q0) * a.G : 0;
+    if (R64 > a.few_rows) return;
+    const int R = (int)R64;
+    int lo, hi;
+    split_range(k1 > k0 ? k1 - k0 : 0, wk.split, a.nsplit, lo, hi);
+    T *dkp = (T *)a.dk + (int64_t)h * a.D, *dvp = (T *)a.dv + (int64_t)h * a.D;
+    if (R == 0) {                                     // keys that nothing attends to
+        float z[4 * VD];
+#pragma unroll
+        for (int e = 0; e < 4 * VD; ++e) z[e] = 0.f;
+        for (int key = k0 + lo + m; key < k0 + hi; key += 16) {
+            store_elems<T, 4 * VD, PB>(dkp + (int64_t)key * a.ld_dk, 4 * g * VD, a.D, z);
+            store_elems<T, 4 * VD, PB>(dvp + (int64_t)key * a.ld_dv, 4 * g * VD, a.D, z);
+        }
+        return;
+    }
+
+    const RowCols<T, DH, PB> rc(g, a.D);
+    const Cols<T, VD, PB> scol(m * VD, a.D);
+    Frag qf[RT][NF], df[RT][NF];
+    Slice<T, DH> qs, os;                              // the rows again, as operands of a contraction over them
+    float lse2[RT], delta[RT], lse2s[8], deltas[8];
+    uint32_t on = 0;                                  // rows that attend to something: bits in stream_of's order
+    f32x4 acc[RT][VD];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int r = 16 * t + m;
+        const Row row = row_at(a, q0, h, r < R ? r : R - 1);
+        const int64_t col = (int64_t)row.head * a.D;
+        Frag of[NF];
+        rc.load(qf[t], (const char *)a.q + (row.query * a.ld_q + col) * ES, 0);
+        rc.load(df[t], (const char *)a.dout + (row.query * a.ld_dout + col) * ES, 0);
+        rc.load(of, (const char *)a.o + (row.query * a.ld_o + col) * ES, 0);
+        rc.clean(qf[t]);
+        rc.clean(df[t]);
+        rc.clean(of);
+        const float lse = a.lse[row.query * a.H + row.head];
+        const bool there = r < R && lse != kNegInf;
+        on |= ((uint32_t)ams_ballot(there) & 0xffffu) << (16 * t);
+        lse2[t] = there ? lse * kLog2e : 0.f;
+        delta[t] = row_delta<T, NF>(df[t], of);
+        delta[t] = there ? delta[t] : 0.f;
+#pragma unroll
+        for (int e = 0; e < VD; ++e) acc[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int r = stream_of(j, g);
+        if (j >= 4 * RT) {                            // the second half of a step, which one tile does not have
+            qs.zero(j);
+            os.zero(j);
+            lse2s[j] = deltas[j] = 0.f;
+            continue;
+        }
+        const Row row = row_at(a, q0, h, r < R ? r : R - 1);
+        const int64_t col = (int64_t)row.head * a.D;
+        scol.load(qs.w[j], (const char *)a.q + (row.query * a.ld_q + col) * ES, 0);
+        scol.load(os.w[j], (const char *)a.dout + (row.query * a.ld_dout + col) * ES, 0);
+        // row r's values are lane r % 16's of tile r / 16
+        lse2s[j] = __shfl(lse2[j >> 2], r & 15, AMS_WAVE);
+        deltas[j] = __shfl(delta[j >> 2], r & 15, AMS_WAVE);
+    }
+    if (on != 0xffffffffu) {
+        qs.keep(on, g);
+        os.keep(on, g);
+    }
+    const float c = a.scale * kLog2e;
+    const uint32_t ldk = (uint32_t)(a.ld_k * ES), ldv = (uint32_t)(a.ld_v * ES);
+    uint32_t krow[2] = {m * ldk, (16 + m) * ldk}, vrow[2] = {m * ldv, (16 + m) * ldv}, srow[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) srow[j] = (uint32_t)stream_of(j, g) * ldk;
+
+    for (int kb = lo; kb < hi; kb += kKeyTile) {
+        Frag kf[2][NF], vf[2][NF];
+        Slice<T, DH> kk;
+        const uint32_t live = live_bits(k0 + kb, k0 + hi, a.mask);
+        if (kb + kKeyTile > hi) {
+            const int last = hi - 1 - kb;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                krow[t] = (uint32_t)min(16 * t + m, last) * ldk;
+                vrow[t] = (uint32_t)min(16 * t + m, last) * ldv;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) srow[j] = (uint32_t)min(stream_of(j, g), last) * ldk;
+        }
+        const char *kp = (const char *)a.k + ((int64_t)(k0 + kb) * a.ld_k + (int64_t)h * a.D) * ES;
+        const char *vp = (const char *)a.v + ((int64_t)(k0 + kb) * a.ld_v + (int64_t)h * a.D) * ES;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            rc.load(kf[t], kp, krow[t]);
+            rc.load(vf[t], vp, vrow[t]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) scol.load(kk.w[j], kp, srow[j]);
+        if (live != 0xffffffffu) kk.keep(live, g);
+
+        // a row per lane: dQ
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float ds[8];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f}, dp = s;
+#pragma unroll
+                for (int f = 0; f < NF; ++f) {
+                    s = mma<T>(kf[t][f], qf[rt][f], s);
+                    dp = mma<T>(vf[t][f], df[rt][f], dp);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(s[r] * c - lse2[rt]);
+                    ds[4 * t + r] = p * (dp[r] - delta[rt]) * a.scale;
+                }
+            }
+            const bool mine = on >> (16 * rt + m) & 1;
+            if (live != 0xffffffffu || on != 0xffffffffu) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    ds[j] = mine && (live >> (4 * g + stream_of(j, 0)) & 1) ? ds[j] : 0.f;
+            }
+            mma_slice<T, DH>(acc[rt], kk, Stream<T>(ds));
+        }
+        // a key per lane: dK and dV
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            float p[8], ds[8];
+#pragma unroll
+            for (int rt = 0; rt < 2; ++rt) {
+                if (rt >= RT) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p[4 + r] = ds[4 + r] = 0.f;
+                    continue;
+                }
+                f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f}, dp = s;
+#pragma unroll
+                for (int f = 0; f < NF; ++f) {
+                    s = mma<T>(qf[rt % RT][f], kf[t][f], s);
+                    dp = mma<T>(df[rt % RT][f], vf[t][f], dp);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int j = 4 * rt + r;
+                    p[j] = __builtin_amdgcn_exp2f(s[r] * c - lse2s[j]);
+                    ds[j] = p[j] * (dp[r] - deltas[j]) * a.scale;
+                }
+            }
+            const bool mine = live >> (16 * t + m) & 1;
+            if (live != 0xffffffffu || on != 0xffffffffu) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool both = mine && (on >> (4 * g + stream_of(j, 0)) & 1);
+                    p[j] = both ? p[j] : 0.f;
+                    ds[j] = both ? ds[j] : 0.f;
+                }
+            }
+            f32x4 ak[VD], av[VD];
+#pragma unroll
+            for (int e = 0; e < VD; ++e) ak[e] = av[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+            mma_slice<T, DH>(ak, qs, Stream<T>(ds));
+            mma_slice<T, DH>(av, os, Stream<T>(p));
+            const int key = kb + 16 * t + m;
+            if (key < hi) {
+                float o[4 * VD];
+                acc_in_order<VD>(ak, 1.f, o);
+                store_elems<T, 4 * VD, PB>(dkp + (int64_t)(k0 + key) * a.ld_dk, 4 * g * VD, a.D, o);
+                acc_in_order<VD>(av, 1.f, o);
+                store_elems<T, 4 * VD, PB>(dvp + (int64_t)(k0 + key) * a.ld_dv, 4 * g * VD, a.D, o);
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int r = 16 * t + m;
+        if (r >= R) continue;
+        const Row row = row_at(a, q0, h, r);
+        float o[4 * VD];
+        acc_in_order<VD>(acc[t], 1.f, o);
+        if (a.nsplit > 1) {
+            float *p = a.part_o + ((int64_t)wk.split * a.n_q * a.H + row.query * a.H + row.head) * a.D;
+#pragma unroll
+            for (int e = 0; e < 4 * VD; ++e)
+                if (4 * g * VD + e < a.D) p[4 * g * VD + e] = o[e];
+        } else {
+            store_elems<T, 4 * VD, PB>((T *)a.dq + row.query * a.ld_dq + (int64_t)row.head * a.D, 4 * g * VD, a.D, o);
+        }
+    }
 }
 
 // Partial sums of the splits added in their order: `per` = 1 (dQ, rows of
@@ -253,32 +555,51 @@ __global__ __launch_bounds__(kAttnThreads) void attn_sum_k(const float *part, in
 // ------------------------------------------------------------------- host
 
 struct Plan {
-    int fwd, dq, dkv;                 // splits
-    int64_t row_tiles, key_tiles;
+    Cut fwd, dq;
+    int few_rows, few_rt, few_split;  // samples of at most few_rows rows go to attn_bwd_few_k (-1: none)
+    int dkv;                          // splits of the rows
+    int64_t key_tiles;
     size_t delta, total;              // workspace: delta's bytes, all
 };
 
-ams_status plan_of(const ams_attn *at, int32_t B, int64_t n_q, int64_t n_k, Plan &p)
+ams_status plan_of(const ams_attn *at, int32_t B, int64_t n_q, int64_t n_k, bool wide, Plan &p)
 {
     const ams_status s = attn_shape(at);
     if (s != AMS_OK) return s;
     const int64_t G = at->n_heads / at->n_kv_heads, Hk = at->n_kv_heads;
     if (B < 0 || n_q < 0 || n_k < 0 || n_q * G > INT32_MAX || n_k > INT32_MAX) return AMS_ERR_SIZE;
-    const int64_t samples = B < 1 ? 1 : B;
-    p.row_tiles = row_tiles(at, B, n_q);
-    p.key_tiles = (n_k >> 6) + B;
-    p.fwd = p.dq = split_count(busy_row_tiles(at, B, n_q), n_k / samples / 128);
+    const int64_t samples = B < 1 ? 1 : B, rows = n_q * G, keys = n_k / samples;
+    p.fwd = p.dq = cut_rows(at, B, n_q, keys, wide);
+    // one pass over the keys where most samples' rows fit one tile
+    p.few_rt = wide && at->head_dim <= 64 && rows > 8 * samples ? 2 : 1;
+    p.few_rows = rows <= 16 * p.few_rt * samples ? 16 * p.few_rt : -1;
+    p.few_split = 1;
+    if (p.few_rows > 0) {
+        p.few_split = split_count((samples * Hk + 3) / 4, keys);      // a wave per split here
+        p.dq.rt = p.few_rt, p.dq.wk = 4, p.dq.nsplit = p.few_split;
+        p.dq.tiles = tiles_of(rows, p.dq.rt == 2 ? 5 : 4, B);
+        p.dq.blocks = p.dq.tiles * Hk * p.dq.nsplit;
+    }
+    p.key_tiles = tiles_of(n_k, 6, B);
     const int64_t kt = (n_k + 63) / 64, ks = n_k < B ? n_k : B;
-    p.dkv = split_count((kt > ks ? kt : ks) * Hk, n_q * G / samples / 32);
-    if (p.row_tiles * Hk * p.fwd > kAttnMaxBlocks || p.key_tiles * Hk * p.dkv > kAttnMaxBlocks) return AMS_ERR_SIZE;
-    const size_t rows = (size_t)n_q * at->n_heads, D = at->head_dim, f = sizeof(float);
-    const size_t fwd = p.fwd > 1 ? align_up(p.fwd * rows * 2 * f) + p.fwd * rows * D * f : 0;
-    const size_t dq = p.dq > 1 ? p.dq * rows * D * f : 0;
+    p.dkv = p.few_rows > 0 ? 1 : split_count((kt > ks ? kt : ks) * Hk, rows / samples);
+    if (p.fwd.blocks > kAttnMaxBlocks || p.dq.blocks > kAttnMaxBlocks || p.key_tiles * Hk * p.dkv > kAttnMaxBlocks)
+        return AMS_ERR_SIZE;
+    const size_t all = (size_t)n_q * at->n_heads, D = at->head_dim, f = sizeof(float);
+    const size_t fwd = p.fwd.nsplit > 1 ? align_up(p.fwd.nsplit * all * 2 * f) + p.fwd.nsplit * all * D * f : 0;
+    const size_t dq = p.dq.nsplit > 1 ? p.dq.nsplit * all * D * f : 0;
     const size_t dkv = p.dkv > 1 ? (size_t)p.dkv * n_k * Hk * 2 * D * f : 0;
-    p.delta = align_up(rows * f);
+    p.delta = align_up(all * f) + 256;              // and any_many
     const size_t bwd = p.delta + (dq > dkv ? dq : dkv);
     p.total = 256 + (fwd > bwd ? fwd : bwd);
     return AMS_OK;
+}
+
+bool strides_ok(int64_t width, std::initializer_list<int64_t> lds)
+{
+    for (int64_t ld : lds)
+        if (ld < width || ld > kAttnMaxStride) return false;
+    return true;
 }
 
 AttnArgs args_of(const ams_attn *at, int32_t B, const int32_t *q_off, int64_t n_q, const int32_t *k_off, int64_t n_k,
@@ -298,8 +619,9 @@ AttnArgs args_of(const ams_attn *at, int32_t B, const int32_t *q_off, int64_t n_
 
 extern "C" size_t ams_xattn_workspace(const ams_attn *attn, int32_t B, int64_t n_q, int64_t n_k)
 {
-    Plan p;
-    return attn && plan_of(attn, B, n_q, n_k, p) == AMS_OK ? p.total : 0;
+    Plan p, q;                         // whichever pieces the call's addresses allow
+    if (!attn || plan_of(attn, B, n_q, n_k, true, p) != AMS_OK || plan_of(attn, B, n_q, n_k, false, q) != AMS_OK) return 0;
+    return p.total > q.total ? p.total : q.total;
 }
 
 extern "C" ams_status ams_xattn_fwd(const ams_attn *attn, int32_t B, const int32_t *q_off, int64_t n_q,
@@ -308,30 +630,32 @@ extern "C" ams_status ams_xattn_fwd(const ams_attn *attn, int32_t B, const int32
                                     int64_t ld_out, float *lse, void *ws, size_t ws_bytes, void *stream)
 {
     if (!attn) return AMS_ERR_NULL;
+    const int64_t ld[] = {ld_q, ld_k, ld_v, ld_out};
+    const void *ptr[] = {q, k, v, out};
+    const int pb = piece_bytes(attn->dtype == AMS_F32 ? 4 : 2, attn->head_dim, 4, ld, ptr);
     Plan pl;
-    const ams_status s = plan_of(attn, B, n_q, n_k, pl);
+    const ams_status s = plan_of(attn, B, n_q, n_k, pb == 16, pl);
     if (s != AMS_OK) return s;
     const int64_t wq = (int64_t)attn->n_heads * attn->head_dim, wk = (int64_t)attn->n_kv_heads * attn->head_dim;
-    if (ld_q < wq || ld_out < wq || ld_k < wk || ld_v < wk) return AMS_ERR_SIZE;
+    if (!strides_ok(wq, {ld_q, ld_out}) || !strides_ok(wk, {ld_k, ld_v})) return AMS_ERR_SIZE;
     if (B == 0 || n_q == 0) return AMS_OK;
     if (!q_off || !k_off || !q || !out || !ws || (n_k > 0 && (!k || !v))) return AMS_ERR_NULL;
     if (ws_bytes < pl.total) return AMS_ERR_WORKSPACE;
     AttnArgs a = args_of(attn, B, q_off, n_q, k_off, n_k, q, ld_q, k, ld_k, v, ld_v, key_mask);
-    a.out = out, a.ld_out = ld_out, a.lse = lse, a.nsplit = pl.fwd;
+    a.out = out, a.ld_out = ld_out, a.lse = lse, a.nsplit = pl.fwd.nsplit, a.tiles = pl.fwd.tiles;
     a.part_ml = (float *)align_up((size_t)ws);
-    a.part_o = (float *)((char *)a.part_ml + align_up((size_t)pl.fwd * n_q * a.H * 2 * sizeof(float)));
+    a.part_o = (float *)((char *)a.part_ml + align_up((size_t)a.nsplit * n_q * a.H * 2 * sizeof(float)));
     hipStream_t st = (hipStream_t)stream;
-    const int64_t ld[] = {ld_q, ld_k, ld_v, ld_out};
-    const void *ptr[] = {q, k, v, out};
-    const int pb = piece_bytes(attn->dtype == AMS_F32 ? 4 : 2, a.D, 4, ld, ptr);
     return with_attn(attn->dtype, a.D, pb, [&](auto t, auto dh, auto piece) {
         using T = decltype(t);
-        const unsigned blocks = (unsigned)(pl.row_tiles * a.Hk * a.nsplit);
-        AMS_LAUNCH("xattn_fwd", st,
-                   attn_fwd_k<T, decltype(dh)::value, decltype(piece)::value, false><<<blocks, kAttnThreads, 0, st>>>(a));
-        if (a.nsplit > 1)
-            AMS_LAUNCH("xattn_join", st,
-                       attn_join_k<T><<<(unsigned)((n_q * a.H + kAttnWaves - 1) / kAttnWaves), kAttnThreads, 0, st>>>(a));
+        constexpr int DH = decltype(dh)::value, PB = decltype(piece)::value;
+        with_cut<T, DH, PB>(pl.fwd, [&](auto rt, auto wk) {
+            AMS_LAUNCH("xattn_fwd", st,
+                       attn_fwd_k<T, DH, PB, false, decltype(rt)::value, decltype(wk)::value>
+                       <<<(unsigned)pl.fwd.blocks, kAttnThreads, 0, st>>>(a));
+            return AMS_OK;
+        });
+        if (a.nsplit > 1) launch_join<T>("xattn_join", a, st);
         return ams_launch_status();
     });
 }
@@ -344,11 +668,14 @@ extern "C" ams_status ams_xattn_bwd(const ams_attn *attn, int32_t B, const int32
                                     int64_t ld_dv, void *ws, size_t ws_bytes, void *stream)
 {
     if (!attn) return AMS_ERR_NULL;
+    const int64_t ld[] = {ld_q, ld_k, ld_v, ld_out, ld_dout, ld_dq, ld_dk, ld_dv};
+    const void *ptr[] = {q, k, v, out, dout, dq, dk, dv};
+    const int pb = piece_bytes(attn->dtype == AMS_F32 ? 4 : 2, attn->head_dim, 8, ld, ptr);
     Plan pl;
-    const ams_status s = plan_of(attn, B, n_q, n_k, pl);
+    const ams_status s = plan_of(attn, B, n_q, n_k, pb == 16, pl);
     if (s != AMS_OK) return s;
     const int64_t wq = (int64_t)attn->n_heads * attn->head_dim, wk = (int64_t)attn->n_kv_heads * attn->head_dim;
-    if (ld_q < wq || ld_out < wq || ld_dout < wq || ld_dq < wq || ld_k < wk || ld_v < wk || ld_dk < wk || ld_dv < wk)
+    if (!strides_ok(wq, {ld_q, ld_out, ld_dout, ld_dq}) || !strides_ok(wk, {ld_k, ld_v, ld_dk, ld_dv}))
         return AMS_ERR_SIZE;
     if (B == 0 || (n_q == 0 && n_k == 0)) return AMS_OK;
     if (!q_off || !k_off || !ws || (n_q > 0 && (!q || !out || !lse || !dout || !dq)) ||
@@ -359,11 +686,12 @@ extern "C" ams_status ams_xattn_bwd(const ams_attn *attn, int32_t B, const int32
     a.o = out, a.ld_o = ld_out, a.lse = (float *)lse, a.dout = dout, a.ld_dout = ld_dout;
     a.dq = dq, a.ld_dq = ld_dq, a.dk = dk, a.ld_dk = ld_dk, a.dv = dv, a.ld_dv = ld_dv;
     a.delta = (float *)align_up((size_t)ws);
+    a.any_many = (int32_t *)((char *)a.delta + pl.delta - 256);
     a.part_o = (float *)((char *)a.delta + pl.delta);
+    a.few_rows = pl.few_rows;
+    // rows of one sample beyond a few: can there be any?
+    const bool many = pl.few_rows < 0 || n_q * a.G > pl.few_rows;
     hipStream_t st = (hipStream_t)stream;
-    const int64_t ld[] = {ld_q, ld_k, ld_v, ld_out, ld_dout, ld_dq, ld_dk, ld_dv};
-    const void *ptr[] = {q, k, v, out, dout, dq, dk, dv};
-    const int pb = piece_bytes(attn->dtype == AMS_F32 ? 4 : 2, a.D, 8, ld, ptr);
     return with_attn(attn->dtype, a.D, pb, [&](auto t, auto dh, auto piece) {
         using T = decltype(t);
         constexpr int DH = decltype(dh)::value, PB = decltype(piece)::value;
@@ -373,16 +701,37 @@ extern "C" ams_status ams_xattn_bwd(const ams_attn *attn, int32_t B, const int32
                        attn_sum_k<T><<<(unsigned)(blocks < 8192 ? blocks : 8192), kAttnThreads, 0, st>>>(
                            a.part_o, a.nsplit, per, heads, a.D, off, B, n, (T *)x0, ld0, (T *)x1, ld1));
         };
+        // beside attn_bwd_few_k usually nothing is left: blocks enough to fill the chip, each with several tiles
+        auto grid = [&](int64_t blocks) { return (unsigned)(pl.few_rows > 0 && blocks > 1024 ? 1024 : blocks); };
+        if (pl.few_rows > 0) {
+            a.nsplit = pl.few_split;
+            const int64_t waves = (int64_t)B * a.Hk * a.nsplit;
+            const unsigned blocks = (unsigned)((waves + kAttnWaves - 1) / kAttnWaves) + 1;
+            auto few = [&](auto rt) {
+                AMS_LAUNCH("xattn_bwd_few", st,
+                           attn_bwd_few_k<T, DH, PB, decltype(rt)::value><<<blocks, kAttnThreads, 0, st>>>(a));
+            };
+            if constexpr (PB == 16 && DH <= 64) {
+                if (pl.few_rt == 2) few(std::integral_constant<int, 2>());
+                else few(std::integral_constant<int, 1>());
+            } else {
+                few(std::integral_constant<int, 1>());
+            }
+        }
         if (n_q > 0) {
-            a.nsplit = pl.dq;
-            AMS_LAUNCH("xattn_dq", st,
-                       attn_dq_k<T, DH, PB><<<(unsigned)(pl.row_tiles * a.Hk * a.nsplit), kAttnThreads, 0, st>>>(a));
+            a.nsplit = pl.dq.nsplit, a.tiles = pl.dq.tiles, a.blocks = pl.dq.blocks;
+            if (many)
+                with_cut<T, DH, PB>(pl.dq, [&](auto rt, auto wk) {
+                    AMS_LAUNCH("xattn_dq", st,
+                               attn_dq_k<T, DH, PB, decltype(rt)::value, decltype(wk)::value>
+                               <<<grid(a.blocks), kAttnThreads, 0, st>>>(a));
+                    return AMS_OK;
+                });
             if (a.nsplit > 1) sum(1, a.H, q_off, n_q, dq, ld_dq, nullptr, 0);
         }
-        if (n_k > 0) {
-            a.nsplit = pl.dkv;
-            AMS_LAUNCH("xattn_dkv", st,
-                       attn_dkv_k<T, DH, PB><<<(unsigned)(pl.key_tiles * a.Hk * a.nsplit), kAttnThreads, 0, st>>>(a));
+        if (n_k > 0 && many) {
+            a.nsplit = pl.dkv, a.blocks = pl.key_tiles * a.Hk * a.nsplit;
+            AMS_LAUNCH("xattn_dkv", st, attn_dkv_k<T, DH, PB><<<grid(a.blocks), kAttnThreads, 0, st>>>(a));
             if (a.nsplit > 1) sum(2, a.Hk, k_off, n_k, dk, ld_dk, dv, ld_dv);
         }
         return ams_launch_status();

@@ -18,8 +18,8 @@
 // operand is read in the same order of keys.  So the probabilities never
 // leave their lane: no transposition, no shared memory, and a row's maximum
 // and sum are one value per lane.  Operands come from memory straight into
-// registers; the four waves of a block take every fourth tile of 32 keys and
-// are joined at the end.
+// registers: short lists are bound by instructions, so a step's addresses are
+// one uniform base and lane offsets that do not change from step to step.
 #pragma once
 
 #include <type_traits>
@@ -81,37 +81,53 @@ inline FastDiv fast_div(uint32_t d)
     return {(uint32_t)(((1ull << 32) * ((1ull << s) - d)) / d + 1), s, d};
 }
 
-// NE elements of a row from element d on, in loads of at most PB bytes (the
-// host picks PB so that every piece is aligned and lies within [0, D) or
-// behind it).  Elements behind D are zero; nothing behind D is read.
-template <class T, int NE, int PB>
-__device__ __forceinline__ void load_elems(uint32_t *dst, const T *row, int d, int D)
-{
-    constexpr int BYTES = NE * (int)sizeof(T), W = BYTES < PB ? BYTES : PB, PE = W / (int)sizeof(T);
+// Byte offsets of NE elements of a row from element d on, in pieces of at most
+// PB bytes (the host picks PB so that every piece is aligned and lies within
+// [0, D) or behind it).  A piece behind D is read at d = 0 instead; `in` says
+// which pieces are there.
+template <class T, int NE, int PB> struct Cols {
+    static constexpr int BYTES = NE * (int)sizeof(T), W = BYTES < PB ? BYTES : PB, PE = W / (int)sizeof(T),
+                         N = BYTES / W, WORDS = BYTES / 4 > 0 ? BYTES / 4 : 1;
+    uint32_t o[N];
+
+    __device__ __forceinline__ Cols() {}
+    __device__ __forceinline__ Cols(int d, int D)
+    {
 #pragma unroll
-    for (int i = 0; i < BYTES / W; ++i) {
-        const int di = d + i * PE;
-        const bool in = di < D;
-        const T *p = row + (in ? di : 0);
-        if constexpr (W == 16) {
-            const uint4 v = *(const uint4 *)p;
-            dst[4 * i] = in ? v.x : 0, dst[4 * i + 1] = in ? v.y : 0;
-            dst[4 * i + 2] = in ? v.z : 0, dst[4 * i + 3] = in ? v.w : 0;
-        } else if constexpr (W == 8) {
-            const uint2 v = *(const uint2 *)p;
-            dst[2 * i] = in ? v.x : 0, dst[2 * i + 1] = in ? v.y : 0;
-        } else if constexpr (W == 4) {
-            const uint32_t v = *(const uint32_t *)p;
-            dst[i] = in ? v : 0;
-        } else {
-            constexpr int PER = 4 / W;                // pieces of a word
-            const uint32_t v = W == 2 ? (uint32_t)*(const uint16_t *)p : (uint32_t)*(const uint8_t *)p;
-            const uint32_t x = in ? v : 0;
-            if (i % PER) dst[i / PER] |= x << (8 * W * (i % PER));
-            else dst[i / PER] = x;
+        for (int i = 0; i < N; ++i) o[i] = d + i * PE < D ? (uint32_t)((d + i * PE) * (int)sizeof(T)) : 0u;
+    }
+    __device__ __forceinline__ void load(uint32_t *dst, const char *base, uint32_t row) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const char *p = base + (row + o[i]);
+            if constexpr (W == 16) {
+                const uint4 v = *(const uint4 *)p;
+                dst[4 * i] = v.x, dst[4 * i + 1] = v.y, dst[4 * i + 2] = v.z, dst[4 * i + 3] = v.w;
+            } else if constexpr (W == 8) {
+                const uint2 v = *(const uint2 *)p;
+                dst[2 * i] = v.x, dst[2 * i + 1] = v.y;
+            } else if constexpr (W == 4) {
+                dst[i] = *(const uint32_t *)p;
+            } else {
+                constexpr int PER = 4 / W;            // pieces of a word
+                const uint32_t v = W == 2 ? (uint32_t)*(const uint16_t *)p : (uint32_t)*(const uint8_t *)p;
+                if (i % PER) dst[i / PER] |= v << (8 * W * (i % PER));
+                else dst[i / PER] = v;
+            }
         }
     }
-}
+    // what lies behind D made zero
+    __device__ __forceinline__ void mask(uint32_t *w, int d, int D) const
+    {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+            if (d + e < D) continue;
+            if constexpr (sizeof(T) == 4) w[e] = 0;
+            else w[e / 2] &= (e & 1) ? 0xffffu : 0xffff0000u;
+        }
+    }
+};
 
 // The reverse: NE floats rounded once to T.
 template <class T, int NE, int PB>
@@ -138,14 +154,31 @@ __device__ __forceinline__ void store_elems(T *row, int d, int D, const float *v
 }
 
 // A row as operand of a contraction over the head width: fragment c of lane
-// group g holds the EP elements from (4 c + g) EP on.
-template <class T, int DH, int PB>
-__device__ __forceinline__ void load_row(Frag *f, const T *row, int g, int D)
-{
-    constexpr int EP = Num<T>::EP;
+// group g holds the EP elements from (4 c + g) EP on.  Of the two rows of a
+// product one is loaded with zeros behind D (`clean`), so that it does not
+// matter what the other one reads there (elements of its own row).
+template <class T, int DH, int PB> struct RowCols {
+    static constexpr int EP = Num<T>::EP, NF = DH / (4 * EP);
+    Cols<T, EP, PB> c[NF];
+    int d0, D;
+
+    __device__ __forceinline__ RowCols(int g, int D_) : d0(g * EP), D(D_)
+    {
 #pragma unroll
-    for (int c = 0; c < DH / (4 * EP); ++c) load_elems<T, EP, PB>(f[c].u, row, (4 * c + g) * EP, D);
-}
+        for (int f = 0; f < NF; ++f) c[f] = Cols<T, EP, PB>(4 * f * EP + d0, D);
+    }
+    __device__ __forceinline__ void load(Frag *f, const char *base, uint32_t row) const
+    {
+#pragma unroll
+        for (int i = 0; i < NF; ++i) c[i].load(f[i].u, base, row);
+    }
+    __device__ __forceinline__ void clean(Frag *f) const
+    {
+        if (D == DH) return;
+#pragma unroll
+        for (int i = 0; i < NF; ++i) c[i].mask(f[i].u, 4 * i * EP + d0, D);
+    }
+};
 
 // Streamed entry j of lane group g within a step of 32 (the order in which
 // both products see the streamed side).
@@ -153,9 +186,19 @@ __device__ __forceinline__ int stream_of(int j, int g) { return 16 * (j >> 2) + 
 
 // The lane's slice of 8 streamed rows, elements (lane % 16) VD .. + VD of
 // each, as raw words: operand of a contraction over the streamed rows.
+// (Elements behind D only reach results behind D, which nobody stores.)
 template <class T, int DH> struct Slice {
     static constexpr int VD = DH / 16, WORDS = VD * (int)sizeof(T) / 4 > 0 ? VD * (int)sizeof(T) / 4 : 1;
     uint32_t w[8][WORDS];
+
+    // entries not in `live` (bits of stream_of's order): whatever they hold (NaN too) must not count
+    __device__ __forceinline__ void keep(uint32_t live, int g)
+    {
+        live >>= 4 * g;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (!(live >> stream_of(j, 0) & 1)) zero(j);
+    }
 
     __device__ __forceinline__ void zero(int j)
     {
@@ -237,6 +280,7 @@ __device__ __forceinline__ float sum_groups(float x)
 
 struct AttnArgs {
     int32_t B, H, Hk, G, D, nsplit;
+    int64_t tiles;                    // of the grid, per key head and split
     FastDiv by_g;
     float scale;
     const int32_t *q_off;
@@ -268,6 +312,9 @@ struct AttnArgs {
     float *delta;
     void *dq, *dk, *dv;
     int64_t ld_dq, ld_dk, ld_dv;
+    int32_t few_rows;                 // samples of at most so many rows are attn_bwd_few_k's (-1: none)
+    int32_t *any_many;                // whether there are others
+    int64_t blocks;                   // of the whole work, where a grid may be smaller
 };
 
 // Last sample i whose first tile, floor(off[i] mul / tile) + own i, is at most
@@ -347,28 +394,58 @@ template <class T> __device__ __forceinline__ void decode4(uint32_t w, uint32_t 
     }
 }
 
+// Which of the 32 entries from `at` on are there: below `end` and, with a
+// mask, kept by it (a bit each, the same in all lanes).
+__device__ __forceinline__ uint32_t live_bits(int at, int end, const uint8_t *mask)
+{
+    const int e = at + (ams_lane() & (kKeyTile - 1));
+    bool on = e < end;
+    if (mask) on = on && mask[on ? e : at] != 0;
+    return (uint32_t)ams_ballot(on);
+}
+
+// Two waves per SIMD where their registers come to 256 or nearly.
+template <class T, int DH, int RT> constexpr int waves_per_simd()
+{
+    return DH * RT * (int)sizeof(T) <= 256 ? 2 : 1;
+}
+
+// The lane's place in a list of rows: tile, key head and split of wave or block `b`.
+struct Work {
+    int split, h;
+    int64_t tile;
+};
+__device__ __forceinline__ Work work_of(int64_t b, const AttnArgs &a)
+{
+    Work w;
+    w.split = (int)(b % a.nsplit);
+    b /= a.nsplit;
+    w.h = (int)(b % a.Hk);
+    w.tile = b / a.Hk;
+    return w;
+}
+
 // ---------------------------------------------------------------- forward
 
-// One block per (row tile, key head, split of the keys).
-template <class T, int DH, int PB, bool PAGED>
-__global__ __launch_bounds__(kAttnThreads) void attn_fwd_k(AttnArgs a)
+// One tile of 16 RT rows per (row tile, key head, split of the keys), by WK
+// waves: with WK = 4 the waves of a block take every fourth step of 32 keys
+// and are joined at the end, with WK = 1 each wave has a tile of its own.
+template <class T, int DH, int PB, bool PAGED, int RT, int WK>
+__global__ __launch_bounds__(kAttnThreads, (waves_per_simd<T, DH, RT>())) void attn_fwd_k(AttnArgs a)
 {
-    constexpr int EP = Num<T>::EP, NF = DH / (4 * EP), VD = DH / 16;
-    constexpr int CB = PB / (int)sizeof(T);           // codes of a piece: as many as elements
-    constexpr int kPad = DH + 4;
-    __shared__ float s_o[kAttnWaves][kRowTile][kPad];
-    __shared__ float s_m[kAttnWaves][kRowTile], s_l[kAttnWaves][kRowTile];
+    constexpr int NF = DH / (4 * Num<T>::EP), VD = DH / 16, ES = (int)sizeof(T);
+    constexpr int CB = PB / ES;                       // codes of a piece: as many as elements
+    constexpr int kRows = kRowTile * RT, kTileShift = RT == 2 ? 5 : 4, kPad = DH + 4;
+    __shared__ float s_o[WK > 1 ? WK : 1][WK > 1 ? kRows : 1][kPad];
+    __shared__ float s_m[WK > 1 ? WK : 1][kRows], s_l[WK > 1 ? WK : 1][kRows];
     const int lane = ams_lane(), m = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);
-    int64_t b = blockIdx.x;
-    const int split = (int)(b % a.nsplit);
-    b /= a.nsplit;
-    const int h = (int)(b % a.Hk);
-    const Span rows = span_of(a.q_off, a.B, a.n_q, a.G, 4, b / a.Hk);
+    const Work wk = work_of(WK == 1 ? (int64_t)blockIdx.x * kAttnWaves + wave : blockIdx.x, a);
+    const int h = wk.h;
+    if (wk.tile >= a.tiles) return;
+    const Span rows = span_of(a.q_off, a.B, a.n_q, a.G, kTileShift, wk.tile);
     const int64_t R = (int64_t)rows.count * a.G;
     if (rows.first < 0 || rows.first >= R) return;
-    const int64_t r_mine = rows.first + m;
-    const Row row = row_at(a, rows.begin, h, (int)(r_mine < R ? r_mine : R - 1));
 
     int k0 = 0, nk;
     const int32_t *pages = nullptr;
@@ -382,196 +459,321 @@ __global__ __launch_bounds__(kAttnThreads) void attn_fwd_k(AttnArgs a)
         nk = k1 > k0 ? k1 - k0 : 0;
     }
     int lo, hi;
-    split_range(nk, split, a.nsplit, lo, hi);
+    split_range(nk, wk.split, a.nsplit, lo, hi);
 
-    Frag qf[NF];
-    load_row<T, DH, PB>(qf, (const T *)a.q + row.query * a.ld_q + (int64_t)row.head * a.D, g, a.D);
-    const float c = a.scale * kLog2e;
-    f32x4 acc[VD];
+    const RowCols<T, DH, PB> rc(g, a.D);
+    Frag qf[RT][NF];
+    Row row[RT];
 #pragma unroll
-    for (int t = 0; t < VD; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float mx = kNegInf, l = 0.f;
+    for (int t = 0; t < RT; ++t) {
+        const int64_t r = rows.first + 16 * t + m;
+        row[t] = row_at(a, rows.begin, h, (int)(r < R ? r : R - 1));
+        rc.load(qf[t], (const char *)a.q + (row[t].query * a.ld_q + (int64_t)row[t].head * a.D) * ES, 0);
+        rc.clean(qf[t]);
+    }
+    const float c = a.scale * kLog2e;
+    f32x4 acc[RT][VD];
+    float mx[RT], l[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int i = 0; i < VD; ++i) acc[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        mx[t] = kNegInf;
+        l[t] = 0.f;
+    }
+    // lane offsets of a step
+    const uint32_t ldk = PAGED ? (uint32_t)a.D : (uint32_t)(a.ld_k * ES);
+    const uint32_t ldv = PAGED ? (uint32_t)a.D : (uint32_t)(a.ld_v * ES);
+    uint32_t krow[2] = {m * ldk, (16 + m) * ldk}, vrow[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) vrow[j] = (uint32_t)(PAGED ? 4 * g + (j & 3) : stream_of(j, g)) * ldv;
+    const Cols<T, VD, PB> vcol(m * VD, a.D);
+    Cols<uint8_t, Num<T>::EP, CB> kc[PAGED ? NF : 1];
+    const Cols<uint8_t, VD, CB> vc(m * VD, a.D);
+    if constexpr (PAGED) {
+#pragma unroll
+        for (int f = 0; f < NF; ++f) kc[f] = Cols<uint8_t, Num<T>::EP, CB>((4 * f + g) * Num<T>::EP, a.D);
+    }
 
-    for (int kb = lo + wave * kKeyTile; kb < hi; kb += kAttnWaves * kKeyTile) {
-        Frag kf[2][NF];
+    // A step's loads, issued a step ahead of their use: behind the last step the
+    // last one's are read again, so that their number never changes.
+    constexpr int kStep = WK * kKeyTile;
+    struct Raw {
+        Frag kf[PAGED ? 1 : 2][PAGED ? 1 : NF];
         Slice<T, DH> vv;
-        bool live[8];
-        float sk[2] = {1.f, 1.f}, sv[2] = {1.f, 1.f};
+        uint32_t kw[2][PAGED ? NF : 1][Num<T>::EP / 4], vw[2][4][(VD + 3) / 4];
+        float sk[2], sv[2];
+        uint32_t there;                               // dense: the lane's mask byte; paged: which halves have a page
+    };
+    auto pages_of = [&](int kb, int *page) {
         if constexpr (PAGED) {
-            const int P1 = (1 << a.page_shift) - 1;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                // 16 consecutive tokens lie in one page; a step's second half behind the last reads the first half's page
+                page[t] = pages[(kb + 16 * t < hi ? kb + 16 * t : kb) >> a.page_shift];
+        }
+    };
+    auto issue = [&](Raw &x, int kb, const int *page) {
+        if constexpr (PAGED) {
+            x.there = 0;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                // 16 consecutive tokens lie in one page; a token behind the last reads the last one
                 const int tok = kb + 16 * t < hi ? kb + 16 * t : kb;
-                const int page = pages[tok >> a.page_shift];
-                const bool ok = page >= 0 && page < a.n_pages;
-                const int64_t at = (int64_t)(ok ? page : 0) * a.Hk + h;
-                sk[t] = a.ks[at];
-                sv[t] = a.vs[at];
-                const uint8_t *kp = a.kc + (at << a.page_shift) * a.D;
-                const uint8_t *vp = a.vc + (at << a.page_shift) * a.D;
-                const int in = tok & P1;
-                {
-                    const uint8_t *r = kp + (int64_t)(in + m) * a.D;
+                const bool ok = page[t] >= 0 && page[t] < a.n_pages;
+                x.there |= ok ? 0xffffu << (16 * t) : 0u;
+                const int64_t at = (int64_t)(ok ? page[t] : 0) * a.Hk + h;
+                x.sk[t] = a.ks[at];
+                x.sv[t] = a.vs[at];
+                const int64_t first = ((at << a.page_shift) + (tok & ((1 << a.page_shift) - 1))) * a.D;
+                const char *kp = (const char *)a.kc + first, *vp = (const char *)a.vc + first;
 #pragma unroll
-                    for (int f = 0; f < NF; ++f) {
-                        uint32_t w[EP / 4];
-                        load_elems<uint8_t, EP, CB>(w, r, (4 * f + g) * EP, a.D);
+                for (int f = 0; f < NF; ++f) kc[f].load(x.kw[t][f], kp, krow[0]);
 #pragma unroll
-                        for (int i = 0; i < EP / 4; ++i) decode4<T>(w[i], kf[t][f].u + i * (int)sizeof(T));
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 4 * t + r;
-                    const uint8_t *p = vp + (int64_t)(in + 4 * g + r) * a.D;
-                    uint32_t w[(VD + 3) / 4], x[8];
-                    load_elems<uint8_t, VD, CB>(w, p, m * VD, a.D);
-#pragma unroll
-                    for (int i = 0; i < (VD + 3) / 4; ++i) decode4<T>(w[i], x + i * (int)sizeof(T));
-#pragma unroll
-                    for (int i = 0; i < Slice<T, DH>::WORDS; ++i) vv.w[j][i] = x[i];
-                    live[j] = ok && kb + stream_of(j, g) < hi;
-                }
+                for (int r = 0; r < 4; ++r) vc.load(x.vw[t][r], vp, vrow[r]);
             }
         } else {
-            const T *kp = (const T *)a.k + (int64_t)h * a.D, *vp = (const T *)a.v + (int64_t)h * a.D;
+            if (kb + kKeyTile > hi) {                 // the last step: what lies behind it reads the last key
+                const int last = hi - 1 - kb;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) krow[t] = (uint32_t)min(16 * t + m, last) * ldk;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) vrow[j] = (uint32_t)min(stream_of(j, g), last) * ldv;
+            }
+            const char *kp = (const char *)a.k + ((int64_t)(k0 + kb) * a.ld_k + (int64_t)h * a.D) * ES;
+            const char *vp = (const char *)a.v + ((int64_t)(k0 + kb) * a.ld_v + (int64_t)h * a.D) * ES;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) rc.load(x.kf[t], kp, krow[t]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) vcol.load(x.vv.w[j], vp, vrow[j]);
+            x.there = 1;
+            if (a.mask) x.there = a.mask[k0 + min(kb + (lane & (kKeyTile - 1)), hi - 1)];
+        }
+    };
+    auto step = [&](Raw &x, int kb) {
+        Frag pf[2][NF];
+        uint32_t live = (uint32_t)ams_ballot(kb + (lane & (kKeyTile - 1)) < hi && (PAGED || x.there != 0));
+        if constexpr (PAGED) {
+            live &= x.there;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                int key = kb + 16 * t + m;
-                key = k0 + (key < hi ? key : hi - 1);
-                load_row<T, DH, PB>(kf[t], kp + (int64_t)key * a.ld_k, g, a.D);
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+#pragma unroll
+                    for (int i = 0; i < Num<T>::EP / 4; ++i) decode4<T>(x.kw[t][f][i], pf[t][f].u + i * ES);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    uint32_t y[8];
+#pragma unroll
+                    for (int i = 0; i < (VD + 3) / 4; ++i) decode4<T>(x.vw[t][r][i], y + i * ES);
+#pragma unroll
+                    for (int i = 0; i < Slice<T, DH>::WORDS; ++i) x.vv.w[4 * t + r][i] = y[i];
+                }
             }
+        }
+        const Frag(*kf)[NF];
+        if constexpr (PAGED) kf = pf;
+        else kf = x.kf;
+        Slice<T, DH> &vv = x.vv;
+        if (live != 0xffffffffu) vv.keep(live, g);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float s[8];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int f = 0; f < NF; ++f) y = mma<T>(kf[t][f], qf[rt][f], y);
+                const float ct = PAGED ? c * x.sk[t] : c;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[4 * t + r] = y[r] * ct;
+            }
+            if (live != 0xffffffffu) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j] = (live >> (4 * g + stream_of(j, 0)) & 1) ? s[j] : kNegInf;
+            }
+            float tm = s[0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) tm = fmaxf(tm, s[j]);
+            tm = max_groups(tm);
+            const float mn = fmaxf(mx[rt], tm), base = mn == kNegInf ? 0.f : mn;
+            const float alpha = __builtin_amdgcn_exp2f(mx[rt] - base);
+            mx[rt] = mn;
+            float p[8], ps = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                int key = kb + stream_of(j, g);
-                live[j] = key < hi;
-                key = k0 + (key < hi ? key : hi - 1);
-                load_elems<T, VD, PB>(vv.w[j], vp + (int64_t)key * a.ld_v, m * VD, a.D);
-                if (a.mask) live[j] = live[j] && a.mask[key] != 0;
+                p[j] = __builtin_amdgcn_exp2f(s[j] - base);
+                ps += p[j];
+            }
+            l[rt] = l[rt] * alpha + ps;
+            if (ams_ballot(alpha != 1.f)) {
+#pragma unroll
+                for (int i = 0; i < VD; ++i) acc[rt][i] *= alpha;
+            }
+            if constexpr (PAGED) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[j] = p[j] == 0.f ? 0.f : p[j] * x.sv[j >> 2];    // a power of two: exact
+            }
+            mma_slice<T, DH>(acc[rt], vv, Stream<T>(p));
+        }
+    };
+    int kb = lo + (WK == 1 ? 0 : wave * kKeyTile);
+    if (kb < hi) {
+        Raw now, then;
+        int page[2] = {0, 0};
+        pages_of(kb, page);
+        issue(now, kb, page);
+        int next = kb + kStep < hi ? kb + kStep : kb;
+        pages_of(next, page);
+        for (;;) {
+            issue(then, next, page);
+            const int after = next + kStep < hi ? next + kStep : next;
+            pages_of(after, page);
+            step(now, kb);
+            if (next == kb) break;
+            kb = next, next = after;
+            now = then;
+        }
+    }
+
+#pragma unroll
+    for (int t = 0; t < RT; ++t) l[t] = sum_groups(l[t]);
+    const int64_t n_rows = a.n_q * a.H;
+    if constexpr (WK == 1) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            if (rows.first + 16 * t + m >= R) continue;
+            const int64_t at = row[t].query * a.H + row[t].head;
+            float o[4 * VD];
+            if (a.nsplit > 1) {
+                const int64_t p = (int64_t)wk.split * n_rows + at;
+                acc_in_order<VD>(acc[t], 1.f, o);
+#pragma unroll
+                for (int i = 0; i < 4 * VD; ++i)
+                    if (4 * g * VD + i < a.D) a.part_o[p * a.D + 4 * g * VD + i] = o[i];
+                if (g == 0) {
+                    a.part_ml[2 * p] = mx[t];
+                    a.part_ml[2 * p + 1] = l[t];
+                }
+            } else {
+                acc_in_order<VD>(acc[t], l[t] == 0.f ? 0.f : 1.f / l[t], o);      // no key: a zero row
+                store_elems<T, 4 * VD, PB>((T *)a.out + row[t].query * a.ld_out + (int64_t)row[t].head * a.D,
+                                           4 * g * VD, a.D, o);
+                if (a.lse && g == 0)
+                    a.lse[at] = l[t] == 0.f ? kNegInf : (mx[t] + __builtin_amdgcn_logf(l[t])) * kLn2;
             }
         }
-        float s[8];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int f = 0; f < NF; ++f) x = mma<T>(kf[t][f], qf[f], x);
-            const float ct = PAGED ? c * sk[t] : c;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) s[4 * t + r] = live[4 * t + r] ? x[r] * ct : kNegInf;
-        }
-        float tm = s[0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) tm = fmaxf(tm, s[j]);
-        tm = max_groups(tm);
-        const float mn = fmaxf(mx, tm), base = mn == kNegInf ? 0.f : mn;
-        const float alpha = __builtin_amdgcn_exp2f(mx - base);
-        mx = mn;
-        float p[8], ps = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            p[j] = __builtin_amdgcn_exp2f(s[j] - base);
-            ps += p[j];
-        }
-        l = l * alpha + ps;
-        if (ams_ballot(alpha != 1.f)) {
-#pragma unroll
-            for (int t = 0; t < VD; ++t) acc[t] *= alpha;
-        }
-        bool all = true;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) all = all && live[j];
-        if (ams_ballot(!all)) {                      // what a masked value holds (NaN too) must not count
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (!live[j]) vv.zero(j);
-        }
-        if constexpr (PAGED) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = live[j] ? p[j] * sv[j >> 2] : 0.f;      // a power of two: exact
-        }
-        mma_slice<T, DH>(acc, vv, Stream<T>(p));
-    }
-
-    // join the four waves
-    l = sum_groups(l);
-    float o[4 * VD];
-    acc_in_order<VD>(acc, 1.f, o);
-#pragma unroll
-    for (int i = 0; i < 4 * VD; ++i) s_o[wave][m][4 * g * VD + i] = o[i];
-    if (g == 0) {
-        s_m[wave][m] = mx;
-        s_l[wave][m] = l;
-    }
-    __syncthreads();
-    const int r = threadIdx.x / 16, d = (threadIdx.x % 16) * VD;
-    const int64_t ro = rows.first + r;
-    if (ro >= R) return;
-    float M = kNegInf, L = 0.f, y[VD];
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) M = fmaxf(M, s_m[w][r]);
-    const float base = M == kNegInf ? 0.f : M;
-#pragma unroll
-    for (int e = 0; e < VD; ++e) y[e] = 0.f;
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(s_m[w][r] - base);
-        L += s_l[w][r] * f;
-#pragma unroll
-        for (int e = 0; e < VD; ++e) y[e] += s_o[w][r][d + e] * f;
-    }
-    const Row ow = row_at(a, rows.begin, h, (int)ro);
-    const int64_t at = ow.query * a.H + ow.head;
-    if (a.nsplit > 1) {
-        const int64_t n_rows = a.n_q * a.H, p = (int64_t)split * n_rows + at;
-        if (threadIdx.x % 16 == 0) {
-            a.part_ml[2 * p] = M;
-            a.part_ml[2 * p + 1] = L;
-        }
-#pragma unroll
-        for (int e = 0; e < VD; ++e)
-            if (d + e < a.D) a.part_o[p * a.D + d + e] = y[e];
         return;
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;       // no key: a zero row
+    // join the four waves
 #pragma unroll
-    for (int e = 0; e < VD; ++e) y[e] *= inv;
-    store_elems<T, VD, PB>((T *)a.out + ow.query * a.ld_out + (int64_t)ow.head * a.D, d, a.D, y);
-    if (a.lse && threadIdx.x % 16 == 0)
-        a.lse[at] = L == 0.f ? kNegInf : (M + __builtin_amdgcn_logf(L)) * kLn2;
+    for (int t = 0; t < RT; ++t) {
+        float o[4 * VD];
+        acc_in_order<VD>(acc[t], 1.f, o);
+#pragma unroll
+        for (int i = 0; i < 4 * VD; ++i) s_o[wave % WK][(16 * t + m) % (WK > 1 ? kRows : 1)][4 * g * VD + i] = o[i];
+        if (g == 0) {
+            s_m[wave % WK][16 * t + m] = mx[t];
+            s_l[wave % WK][16 * t + m] = l[t];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int r = 16 * t + threadIdx.x / 16, d = (threadIdx.x % 16) * VD;
+        const int64_t ro = rows.first + r;
+        if (ro >= R) return;
+        float M = kNegInf, L = 0.f, y[VD];
+#pragma unroll
+        for (int w = 0; w < WK; ++w) M = fmaxf(M, s_m[w][r]);
+        const float base = M == kNegInf ? 0.f : M;
+#pragma unroll
+        for (int e = 0; e < VD; ++e) y[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < WK; ++w) {
+            const float f = __builtin_amdgcn_exp2f(s_m[w][r] - base);
+            L += s_l[w][r] * f;
+#pragma unroll
+            for (int e = 0; e < VD; ++e) y[e] += s_o[w][r % (WK > 1 ? kRows : 1)][d + e] * f;
+        }
+        const Row ow = row_at(a, rows.begin, h, (int)ro);
+        const int64_t at = ow.query * a.H + ow.head;
+        if (a.nsplit > 1) {
+            const int64_t p = (int64_t)wk.split * n_rows + at;
+            if (threadIdx.x % 16 == 0) {
+                a.part_ml[2 * p] = M;
+                a.part_ml[2 * p + 1] = L;
+            }
+#pragma unroll
+            for (int e = 0; e < VD; ++e)
+                if (d + e < a.D) a.part_o[p * a.D + d + e] = y[e];
+            continue;
+        }
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+        for (int e = 0; e < VD; ++e) y[e] *= inv;
+        store_elems<T, VD, PB>((T *)a.out + ow.query * a.ld_out + (int64_t)ow.head * a.D, d, a.D, y);
+        if (a.lse && threadIdx.x % 16 == 0)
+            a.lse[at] = L == 0.f ? kNegInf : (M + __builtin_amdgcn_logf(L)) * kLn2;
+    }
 }
 
-// The splits of the keys joined: one wave per (query, head).
-template <class T>
+// The splits of the keys joined: one block per (query, head), or four of them
+// with a wave each (W = 1) where the splits are few.
+template <class T, int W>
 __global__ __launch_bounds__(kAttnThreads) void attn_join_k(AttnArgs a)
 {
-    const int lane = ams_lane();
-    const int64_t at = (int64_t)blockIdx.x * kAttnWaves + threadIdx.x / AMS_WAVE, n_rows = a.n_q * a.H;
+    __shared__ float s_y[W][2 * AMS_WAVE], s_l[W];
+    const int lane = ams_lane(), wave = threadIdx.x / AMS_WAVE;
+    const int64_t at = W == 1 ? (int64_t)blockIdx.x * kAttnWaves + wave : blockIdx.x, n_rows = a.n_q * a.H;
     if (at >= n_rows) return;
     const int64_t query = at / a.H;
-    const int head = (int)(at % a.H);
+    const int head = (int)(at - query * a.H);
     if (query < clamp_off(a.q_off[0], a.n_q) || query >= clamp_off(a.q_off[a.B], a.n_q)) return;   // no sample's row
     float M = kNegInf;
     for (int s = lane; s < a.nsplit; s += AMS_WAVE) M = fmaxf(M, a.part_ml[2 * (s * n_rows + at)]);
     M = ams_wave_max(M);
     const float base = M == kNegInf ? 0.f : M;
     float L = 0.f, y0 = 0.f, y1 = 0.f;
-    const bool in0 = lane < a.D, in1 = lane + AMS_WAVE < a.D;
-#pragma unroll 4
-    for (int s = 0; s < a.nsplit; ++s) {
+    const int d0 = lane < a.D ? lane : 0, d1 = lane + AMS_WAVE < a.D ? lane + AMS_WAVE : 0;
+#pragma unroll 8
+    for (int s = W == 1 ? 0 : wave; s < a.nsplit; s += W) {
         const int64_t p = s * n_rows + at;
-        const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * p] - base);
-        L += a.part_ml[2 * p + 1] * f;
-        if (in0) y0 += a.part_o[p * a.D + lane] * f;
-        if (in1) y1 += a.part_o[p * a.D + lane + AMS_WAVE] * f;
+        const float m = a.part_ml[2 * p], l = a.part_ml[2 * p + 1];
+        const float x0 = a.part_o[p * a.D + d0], x1 = a.part_o[p * a.D + d1];
+        const float f = __builtin_amdgcn_exp2f(m - base);
+        L += l * f;
+        y0 += x0 * f;
+        y1 += x1 * f;
+    }
+    if constexpr (W > 1) {
+        s_y[wave][lane] = y0;
+        s_y[wave][AMS_WAVE + lane] = y1;
+        if (lane == 0) s_l[wave] = L;
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int w = 1; w < W; ++w) {
+            y0 += s_y[w][lane];
+            y1 += s_y[w][AMS_WAVE + lane];
+            L += s_l[w];
+        }
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;
     T *out = (T *)a.out + query * a.ld_out + (int64_t)head * a.D;
     y0 *= inv, y1 *= inv;
-    if (in0) store_elems<T, 1, (int)sizeof(T)>(out, lane, a.D, &y0);
-    if (in1) store_elems<T, 1, (int)sizeof(T)>(out, lane + AMS_WAVE, a.D, &y1);
+    if (lane < a.D) store_elems<T, 1, (int)sizeof(T)>(out, lane, a.D, &y0);
+    if (lane + AMS_WAVE < a.D) store_elems<T, 1, (int)sizeof(T)>(out, lane + AMS_WAVE, a.D, &y1);
     if (a.lse && lane == 0) a.lse[at] = L == 0.f ? kNegInf : (M + __builtin_amdgcn_logf(L)) * kLn2;
+}
+
+template <class T> void launch_join(const char *name, const AttnArgs &a, hipStream_t st)
+{
+    const int64_t n = a.n_q * a.H;
+    if (a.nsplit >= 8)
+        AMS_LAUNCH(name, st, attn_join_k<T, kAttnWaves><<<(unsigned)n, kAttnThreads, 0, st>>>(a));
+    else
+        AMS_LAUNCH(name, st,
+                   attn_join_k<T, 1><<<(unsigned)((n + kAttnWaves - 1) / kAttnWaves), kAttnThreads, 0, st>>>(a));
 }
 
 // ------------------------------------------------------------------- host
@@ -588,31 +790,53 @@ inline ams_status attn_shape(const ams_attn *at)
     return AMS_OK;
 }
 
-// Row tiles of all samples (each sample's own number is not known here).
-inline int64_t row_tiles(const ams_attn *at, int32_t B, int64_t n_q)
-{
-    return (n_q * (at->n_heads / at->n_kv_heads) >> 4) + B;
-}
+constexpr int64_t kAttnMaxStride = 1 << 24;            // 32 rows' bytes fit the lanes' 32-bit offsets
 
-// Splits of the streamed side so that about two blocks per compute unit are
-// there: `tiles` are the tiles with work, `steps` the steps of 128 entries
-// (one per wave) that a tile's share has on average.  One while there are
-// 384 blocks without it; a split keeps two such steps at least, below which
-// its partial sums cost more than it saves.
-inline int split_count(int64_t tiles, int64_t steps)
+// How a forward call (or dQ's) is cut.
+struct Cut {
+    int rt, wk, nsplit;
+    int64_t tiles, blocks;
+};
+
+// Tiles of `rows` streamed against per sample: floor(n / size) + B of them are
+// launched (each sample's own number is not known here).
+inline int64_t tiles_of(int64_t n, int shift, int32_t B) { return (n >> shift) + B; }
+
+// Splits of the streamed side when `tiles` blocks have work: up to two blocks
+// per compute unit while a split keeps 256 entries (two steps of the block;
+// below that its partial sums cost more than it saves), up to four with 1536
+// (measured: 3 queries over 80,000 keys, 8 heads of 128, 188 us at 21 splits
+// and 171 at 42; 32 queries over 2,300 8-bit tokens, 8 key heads, 51 us at 2
+// splits and 53 at 4).
+inline int split_count(int64_t tiles, int64_t entries)
 {
     if (tiles < 1) tiles = 1;
-    if (tiles >= 384) return 1;
-    int64_t n = 512 / tiles;
-    if (n > steps / 2) n = steps / 2;
-    if (n > 256) n = 256;
-    return n < 1 ? 1 : (int)n;
+    const int64_t two = 512 / tiles < entries / 256 ? 512 / tiles : entries / 256;
+    const int64_t four = 1024 / tiles < entries / 1536 ? 1024 / tiles : entries / 1536;
+    const int64_t n = two > four ? two : four;
+    return n < 1 ? 1 : (n > 256 ? 256 : (int)n);
 }
 
-inline int64_t busy_row_tiles(const ams_attn *at, int32_t B, int64_t n_q)
+// rows: all samples' rows of one key head; keys: a sample's (on average).
+// Two row tiles per wave once a sample has more than one on average (the keys
+// are read and unpacked once for both), where the registers allow it.
+inline Cut cut_rows(const ams_attn *at, int32_t B, int64_t n_q, int64_t keys, bool wide)
 {
-    const int64_t t = (n_q * (at->n_heads / at->n_kv_heads) + 15) / 16, s = n_q < B ? n_q : B;
-    return (t > s ? t : s) * at->n_kv_heads;
+    const int64_t rows = n_q * (at->n_heads / at->n_kv_heads), Hk = at->n_kv_heads;
+    const int64_t samples = B < 1 ? 1 : B;
+    Cut c;
+    c.rt = wide && rows > 16 * samples && (at->dtype == AMS_BF16 || at->head_dim <= 64) ? 2 : 1;
+    const int shift = c.rt == 2 ? 5 : 4;
+    c.tiles = tiles_of(rows, shift, B);
+    int64_t busy = (rows + (1 << shift) - 1) >> shift;
+    const int64_t with_rows = n_q < B ? n_q : B;
+    busy = (busy > with_rows ? busy : with_rows) * Hk;
+    // short lists and many of them: a wave per tile, nothing to join
+    c.wk = keys <= 256 && busy >= 1024 ? 1 : 4;
+    c.nsplit = c.wk == 1 ? 1 : split_count(busy, keys);
+    const int64_t work = c.tiles * Hk * c.nsplit;
+    c.blocks = c.wk == 1 ? (work + kAttnWaves - 1) / kAttnWaves : work;
+    return c;
 }
 
 // Widest load (16, 8 or one element's bytes) for which a row's width, its
@@ -640,6 +864,19 @@ template <class F> ams_status with_attn(int32_t dtype, int32_t D, int pb, F f)
     if (pb == 16) return dims((uint16_t)0, std::integral_constant<int, 16>());
     if (pb == 8) return dims((uint16_t)0, std::integral_constant<int, 8>());
     return dims((uint16_t)0, std::integral_constant<int, 2>());
+}
+
+// f(RT, WK): two row tiles only in the widest pieces, and not for 128 floats
+// (whose operands alone would fill the registers).
+template <class T, int DH, int PB, class F> ams_status with_cut(const Cut &c, F f)
+{
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    using Four = std::integral_constant<int, 4>;
+    if constexpr (PB == 16 && (sizeof(T) == 2 || DH <= 64)) {
+        if (c.rt == 2) return c.wk == 1 ? f(Two(), One()) : f(Two(), Four());
+    }
+    return c.wk == 1 ? f(One(), One()) : f(One(), Four());
 }
 
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }

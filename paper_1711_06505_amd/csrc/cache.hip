@@ -169,7 +169,7 @@ ams_status cache_shape(const ams_cache *c, int &page_shift)
     return AMS_OK;
 }
 
-ams_status read_plan(const ams_attn *at, const ams_cache *c, int32_t B, int64_t n_q, int &nsplit, size_t &total)
+ams_status read_plan(const ams_attn *at, const ams_cache *c, int32_t B, int64_t n_q, bool wide, Cut &cut, size_t &total)
 {
     ams_status s = attn_shape(at);
     int shift;
@@ -177,11 +177,12 @@ ams_status read_plan(const ams_attn *at, const ams_cache *c, int32_t B, int64_t 
     if (s != AMS_OK) return s;
     if (at->n_kv_heads != c->n_kv_heads || at->head_dim != c->head_dim) return AMS_ERR_DIMS;
     if (B < 0 || n_q < 0 || n_q * (at->n_heads / at->n_kv_heads) > INT32_MAX) return AMS_ERR_SIZE;
-    nsplit = split_count(busy_row_tiles(at, B, n_q), (int64_t)c->max_pages * c->page / 128);
-    if (row_tiles(at, B, n_q) * at->n_kv_heads * nsplit > kAttnMaxBlocks) return AMS_ERR_SIZE;
+    cut = cut_rows(at, B, n_q, (int64_t)c->max_pages * c->page, wide);
+    if (cut.blocks > kAttnMaxBlocks) return AMS_ERR_SIZE;
     const size_t rows = (size_t)n_q * at->n_heads;
     total = 256;
-    if (nsplit > 1) total += align_up(nsplit * rows * 2 * sizeof(float)) + nsplit * rows * at->head_dim * sizeof(float);
+    if (cut.nsplit > 1)
+        total += align_up(cut.nsplit * rows * 2 * sizeof(float)) + cut.nsplit * rows * at->head_dim * sizeof(float);
     return AMS_OK;
 }
 
@@ -229,9 +230,12 @@ extern "C" ams_status ams_cache_write(const ams_cache *cache, int32_t dtype, int
 
 extern "C" size_t ams_cache_workspace(const ams_attn *attn, const ams_cache *cache, int32_t B, int64_t n_q)
 {
-    int nsplit;
-    size_t total;
-    return attn && cache && read_plan(attn, cache, B, n_q, nsplit, total) == AMS_OK ? total : 0;
+    Cut cut;
+    size_t a, b;                       // whichever pieces the call's addresses allow
+    if (!attn || !cache || read_plan(attn, cache, B, n_q, true, cut, a) != AMS_OK ||
+        read_plan(attn, cache, B, n_q, false, cut, b) != AMS_OK)
+        return 0;
+    return a > b ? a : b;
 }
 
 extern "C" ams_status ams_cache_attn(const ams_attn *attn, const ams_cache *cache, int32_t B, const int32_t *q_off,
@@ -242,8 +246,15 @@ extern "C" ams_status ams_cache_attn(const ams_attn *attn, const ams_cache *cach
 {
     if (!attn || !cache) return AMS_ERR_NULL;
     AttnArgs a{};
+    const int64_t ld[] = {ld_q, ld_out};
+    const void *ptr[] = {q, out};
+    const int es = attn->dtype == AMS_F32 ? 4 : 2;
+    int pb = piece_bytes(es, attn->head_dim, 2, ld, ptr);
+    const uint64_t codes = (uint64_t)(uintptr_t)k_codes | (uint64_t)(uintptr_t)v_codes;
+    if (codes & (pb / es - 1)) pb = es;                // a piece of codes has as many entries as one of q
+    Cut cut;
     size_t total;
-    const ams_status s = read_plan(attn, cache, B, n_q, a.nsplit, total);
+    const ams_status s = read_plan(attn, cache, B, n_q, pb == 16, cut, total);
     if (s != AMS_OK) return s;
     cache_shape(cache, a.page_shift);
     const int64_t w = (int64_t)attn->n_heads * attn->head_dim;
@@ -260,22 +271,19 @@ extern "C" ams_status ams_cache_attn(const ams_attn *attn, const ams_cache *cach
     a.kc = k_codes, a.vc = v_codes, a.ks = k_scale, a.vs = v_scale;
     a.out = out, a.ld_out = ld_out, a.lse = lse;
     a.part_ml = (float *)align_up((size_t)ws);
-    a.part_o = (float *)((char *)a.part_ml + align_up((size_t)a.nsplit * n_q * a.H * 2 * sizeof(float)));
+    a.part_o = (float *)((char *)a.part_ml + align_up((size_t)cut.nsplit * n_q * a.H * 2 * sizeof(float)));
     hipStream_t st = (hipStream_t)stream;
-    const int64_t ld[] = {ld_q, ld_out};
-    const void *ptr[] = {q, out};
-    const int es = attn->dtype == AMS_F32 ? 4 : 2;
-    int pb = piece_bytes(es, a.D, 2, ld, ptr);
-    const uint64_t codes = (uint64_t)(uintptr_t)k_codes | (uint64_t)(uintptr_t)v_codes;
-    if (codes & (pb / es - 1)) pb = es;                // a piece of codes has as many entries as one of q
+    a.nsplit = cut.nsplit, a.tiles = cut.tiles;
     return with_attn(attn->dtype, a.D, pb, [&](auto t, auto dh, auto piece) {
         using T = decltype(t);
-        const unsigned blocks = (unsigned)(row_tiles(attn, B, n_q) * a.Hk * a.nsplit);
-        AMS_LAUNCH("cache_attn", st,
-                   attn_fwd_k<T, decltype(dh)::value, decltype(piece)::value, true><<<blocks, kAttnThreads, 0, st>>>(a));
-        if (a.nsplit > 1)
-            AMS_LAUNCH("cache_join", st,
-                       attn_join_k<T><<<(unsigned)((n_q * a.H + kAttnWaves - 1) / kAttnWaves), kAttnThreads, 0, st>>>(a));
+        constexpr int DH = decltype(dh)::value, PB = decltype(piece)::value;
+        with_cut<T, DH, PB>(cut, [&](auto rt, auto wk) {
+            AMS_LAUNCH("cache_attn", st,
+                       attn_fwd_k<T, DH, PB, true, decltype(rt)::value, decltype(wk)::value>
+                       <<<(unsigned)cut.blocks, kAttnThreads, 0, st>>>(a));
+            return AMS_OK;
+        });
+        if (a.nsplit > 1) launch_join<T>("cache_join", a, st);
         return ams_launch_status();
     });
 }
