@@ -12,6 +12,7 @@
 #include <initializer_list>
 
 #include "attn_device.h"
+#include "attn_many.h"
 
 namespace {
 
@@ -554,8 +555,12 @@ __global__ __launch_bounds__(kAttnThreads) void attn_sum_k(const float *part, in
 
 // ------------------------------------------------------------------- host
 
+// Rows of a sample, on average, from which the 32-row kernels are the faster ones.
+constexpr int64_t kManyFrom = 64;
+
 struct Plan {
     Cut fwd, dq;
+    bool many;                        // the kernels of attn_many.h
     int few_rows, few_rt, few_split;  // samples of at most few_rows rows go to attn_bwd_few_k (-1: none)
     int dkv;                          // splits of the rows
     int64_t key_tiles;
@@ -570,6 +575,14 @@ ams_status plan_of(const ams_attn *at, int32_t B, int64_t n_q, int64_t n_k, bool
     if (B < 0 || n_q < 0 || n_k < 0 || n_q * G > INT32_MAX || n_k > INT32_MAX) return AMS_ERR_SIZE;
     const int64_t samples = B < 1 ? 1 : B, rows = n_q * G, keys = n_k / samples;
     p.fwd = p.dq = cut_rows(at, B, n_q, keys, wide);
+    p.many = wide && at->dtype == AMS_BF16 && rows >= kManyFrom * samples;
+    if (p.many) {
+        int64_t busy = (rows + kManyRows - 1) >> kManyShift;
+        if (busy < samples) busy = samples;
+        p.fwd.nsplit = p.dq.nsplit = split_count(busy * Hk, keys);
+        p.fwd.tiles = p.dq.tiles = tiles_of(rows, kManyShift, B);
+        p.fwd.blocks = p.dq.blocks = p.fwd.tiles * Hk * p.fwd.nsplit;
+    }
     // one pass over the keys where most samples' rows fit one tile
     p.few_rt = wide && at->head_dim <= 64 && rows > 8 * samples ? 2 : 1;
     p.few_rows = rows <= 16 * p.few_rt * samples ? 16 * p.few_rt : -1;
@@ -580,8 +593,9 @@ ams_status plan_of(const ams_attn *at, int32_t B, int64_t n_q, int64_t n_k, bool
         p.dq.tiles = tiles_of(rows, p.dq.rt == 2 ? 5 : 4, B);
         p.dq.blocks = p.dq.tiles * Hk * p.dq.nsplit;
     }
-    p.key_tiles = tiles_of(n_k, 6, B);
-    const int64_t kt = (n_k + 63) / 64, ks = n_k < B ? n_k : B;
+    const int key_shift = p.many ? kManyShift : 6;
+    p.key_tiles = tiles_of(n_k, key_shift, B);
+    const int64_t kt = (n_k + (1 << key_shift) - 1) >> key_shift, ks = n_k < B ? n_k : B;
     p.dkv = p.few_rows > 0 ? 1 : split_count((kt > ks ? kt : ks) * Hk, rows / samples);
     if (p.fwd.blocks > kAttnMaxBlocks || p.dq.blocks > kAttnMaxBlocks || p.key_tiles * Hk * p.dkv > kAttnMaxBlocks)
         return AMS_ERR_SIZE;
@@ -649,6 +663,14 @@ extern "C" ams_status ams_xattn_fwd(const ams_attn *attn, int32_t B, const int32
     return with_attn(attn->dtype, a.D, pb, [&](auto t, auto dh, auto piece) {
         using T = decltype(t);
         constexpr int DH = decltype(dh)::value, PB = decltype(piece)::value;
+        if constexpr (PB == 16 && sizeof(T) == 2) {
+            if (pl.many) {
+                AMS_LAUNCH("xattn_fwd_many", st,
+                           attn_fwd_many_k<DH><<<(unsigned)pl.fwd.blocks, kAttnThreads, 0, st>>>(a));
+                if (a.nsplit > 1) launch_join<T>("xattn_join", a, st);
+                return ams_launch_status();
+            }
+        }
         with_cut<T, DH, PB>(pl.fwd, [&](auto rt, auto wk) {
             AMS_LAUNCH("xattn_fwd", st,
                        attn_fwd_k<T, DH, PB, false, decltype(rt)::value, decltype(wk)::value>
@@ -701,6 +723,23 @@ extern "C" ams_status ams_xattn_bwd(const ams_attn *attn, int32_t B, const int32
                        attn_sum_k<T><<<(unsigned)(blocks < 8192 ? blocks : 8192), kAttnThreads, 0, st>>>(
                            a.part_o, a.nsplit, per, heads, a.D, off, B, n, (T *)x0, ld0, (T *)x1, ld1));
         };
+        if constexpr (PB == 16 && sizeof(T) == 2) {
+            if (pl.many) {
+                if (n_q > 0) {
+                    a.nsplit = pl.dq.nsplit, a.tiles = pl.dq.tiles;
+                    AMS_LAUNCH("xattn_dq_many", st,
+                               attn_dq_many_k<DH><<<(unsigned)pl.dq.blocks, kAttnThreads, 0, st>>>(a));
+                    if (a.nsplit > 1) sum(1, a.H, q_off, n_q, dq, ld_dq, nullptr, 0);
+                }
+                if (n_k > 0) {
+                    a.nsplit = pl.dkv, a.tiles = pl.key_tiles;
+                    AMS_LAUNCH("xattn_dkv_many", st,
+                               attn_dkv_many_k<DH><<<(unsigned)(pl.key_tiles * a.Hk * a.nsplit), kAttnThreads, 0, st>>>(a));
+                    if (a.nsplit > 1) sum(2, a.Hk, k_off, n_k, dk, ld_dk, dv, ld_dv);
+                }
+                return ams_launch_status();
+            }
+        }
         // beside attn_bwd_few_k usually nothing is left: blocks enough to fill the chip, each with several tiles
         auto grid = [&](int64_t blocks) { return (unsigned)(pl.few_rows > 0 && blocks > 1024 ? 1024 : blocks); };
         if (pl.few_rows > 0) {

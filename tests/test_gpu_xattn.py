@@ -88,7 +88,7 @@ class Problem:
             k = k.repeat_interleave(self.H // self.Hk, 1)[on]
             s = torch.einsum("qhd,khd->qhk", q, k) * self.attn.scale
             want = torch.logsumexp(s, 2) if k.shape[0] else torch.full((a, self.H), -np.inf, dtype=torch.float64)
-            big = torch.einsum("qhd,khd->qhk", q.abs(), k.abs()).amax(2) * self.attn.scale if k.shape[0] else 0
+            big = torch.einsum("qhd,khd->qhk", q.abs(), k.abs()).amax(2) * abs(self.attn.scale) if k.shape[0] else 0
             if k.shape[0]:
                 tol = (self.D + 12) * attn_ref.U * big + (b + 20) * attn_ref.U * (1 + want.abs())
                 assert ((lse[q0:q0 + a] - want).abs() <= tol).all()
@@ -124,6 +124,36 @@ def test_against_float64(shape, dtype):
     Problem(*shape, dtype).check()
 
 
+MANY = [                                     # samples of many rows: several tiles of rows and of keys
+    ([128], [64], 1, 1, 64), ([129, 70], [65, 127], 4, 2, 128), ([33, 260, 0], [300, 1, 9], 8, 2, 64),
+    ([257], [513], 2, 1, 32), ([100], [1000], 4, 1, 128), ([90, 90], [5, 0], 2, 2, 96), ([150], [190], 3, 1, 40),
+    ([700], [300], 2, 2, 72), ([70], [2500], 2, 1, 64), ([1500], [130], 2, 2, 16), ([64, 64], [64, 128], 5, 1, 8)]
+
+
+@pytest.mark.parametrize("drop", [0.0, 0.4])
+@pytest.mark.parametrize("shape", MANY, ids=lambda s: f"q{sum(s[0])}k{sum(s[1])}h{s[2]}_{s[3]}d{s[4]}")
+def test_many_rows(shape, drop):
+    p = Problem(*shape, "bf16", drop=drop, seed=13, extra=8)
+    if drop:
+        p.k[p.mask == 0] = float("nan")
+        p.v[p.mask == 0] = float("nan")
+    p.check()
+    if shape[4] == 64:
+        Problem(*shape, "f32", drop=drop, seed=14).check()
+
+
+def test_many_rows_without_a_key():
+    """Every key of one sample masked: zero rows, whatever the upstream gradient holds there."""
+    p = Problem([100, 80], [90, 70], 2, 1, 64, "bf16", seed=15, drop=0.1)
+    p.mask[:90] = 0
+    p.k[:90] = float("nan")
+    p.do[:100] = float("nan")
+    out, lse = p.forward()
+    dq, dk, dv = p.backward(out, lse)
+    assert (out[:100] == 0).all() and (dq[:100] == 0).all() and (dk[:90] == 0).all() and (dv[:90] == 0).all()
+    assert all(torch.isfinite(x.float()).all() for x in (out, dq[100:180], dk[90:160], dv[90:160]))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("drop", [0.3, 0.97, 1.0])
 def test_key_mask(drop, dtype):
@@ -141,6 +171,16 @@ def test_key_mask(drop, dtype):
 @pytest.mark.parametrize("D", [12, 64])
 def test_strides_and_alignment(D, extra, offset, dtype):
     Problem([5, 1, 18], [70, 300, 2], 4, 2, D, dtype, extra=extra, offset=offset, seed=2).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scales(dtype):
+    """A negative scale, and one of zero (equal weights), for few and many rows."""
+    for scale in (-0.3, 0.0):
+        for shape in (([3, 2], [40, 70], 2, 2, 16), ([200], [150], 2, 1, 64)):
+            p = Problem(*shape, dtype, seed=8)
+            p.attn.scale = scale
+            p.check()
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
