@@ -25,6 +25,18 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
+typedef __attribute__((address_space(3))) void lds_bytes;
+
+// All of this wave's loads into shared memory and its reads of it done: before
+// the barrier after which others read the one and overwrite the other.
+__device__ __forceinline__ void staged()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x7 << 4);             // vmcnt 0, lgkmcnt 0
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 constexpr int kManyRows = 128;        // rows (keys) of a block, 32 a wave
 constexpr int kManyShift = 7;
 constexpr int kManyStep = 64;         // streamed entries of a tile
@@ -100,40 +112,105 @@ __device__ __forceinline__ Work many_work(int64_t b, const AttnArgs &a)
     return w;
 }
 
-// The keys' side: 64 of K and V, a step ahead in registers, then in shared memory.
-template <int DH> struct KeyStage {
+// A tile's way into shared memory: loads that put their 16 bytes there
+// themselves, lane by lane, so the permutation is made on the source side.
+// What lies behind D or behind the last row reads another piece of the tile:
+// the first meets zeros of the other operand or results that nobody stores,
+// the second weights of zero.
+template <int DH> struct Dma {
     using TL = Tile<DH>;
-    uint4 k[TL::kPer], v[TL::kPer];
-    uint64_t live, next_live;
+    uint32_t off[TL::kPer];
 
-    __device__ __forceinline__ void load(const AttnArgs &a, int h, int k0, int kb, int hi)
+    __device__ static __forceinline__ int slot(int i)
     {
-        const int lane = ams_lane(), last = hi - 1 - kb;
-        bool on = kb + lane < hi;
-        if (a.mask) on = on && a.mask[k0 + (on ? kb + lane : kb)] != 0;
-        next_live = ams_ballot(on);
-        const char *kp = (const char *)a.k + ((int64_t)(k0 + kb) * a.ld_k + (int64_t)h * a.D) * 2;
-        const char *vp = (const char *)a.v + ((int64_t)(k0 + kb) * a.ld_v + (int64_t)h * a.D) * 2;
-#pragma unroll
-        for (int i = 0; i < TL::kPer; ++i) {
-            const int at = i * kAttnThreads + threadIdx.x, row = at / TL::kPieces, piece = at % TL::kPieces;
-            const uint32_t r = (uint32_t)min(row, last), col = piece * 8 < a.D ? piece * 16 : 0;
-            k[i] = *(const uint4 *)(kp + (r * (uint32_t)(a.ld_k * 2) + col));
-            v[i] = *(const uint4 *)(vp + (r * (uint32_t)(a.ld_v * 2) + col));
-        }
+        return (__builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE) * TL::kPer + i) * AMS_WAVE + ams_lane();
     }
-    // entries that take no part as zeros, whatever they hold
-    __device__ __forceinline__ void store(const AttnArgs &a, char *kt, char *vt)
+    __device__ static __forceinline__ int row(int i) { return slot(i) / TL::kPieces; }
+    __device__ static __forceinline__ uint32_t col(int i, int D)
     {
-        live = next_live;
-        const bool whole = live == ~0ull && a.D == DH;
+        const int r = row(i), piece = (slot(i) % TL::kPieces) ^ TL::swizzle(r);
+        return piece * 8 < D ? piece * 16 : 0;
+    }
+    __device__ __forceinline__ void rows(int last, uint32_t ld, int D)        // of a plain list
+    {
 #pragma unroll
-        for (int i = 0; i < TL::kPer; ++i) {
-            const int at = i * kAttnThreads + threadIdx.x, row = at / TL::kPieces, piece = at % TL::kPieces;
-            if (!whole && !((live >> row & 1) && piece * 8 < a.D)) k[i] = v[i] = make_uint4(0, 0, 0, 0);
-            *(uint4 *)(kt + TL::at(row, piece)) = k[i];
-            *(uint4 *)(vt + TL::at(row, piece)) = v[i];
+        for (int i = 0; i < TL::kPer; ++i) off[i] = (uint32_t)min(row(i), last) * ld + col(i, D);
+    }
+    __device__ __forceinline__ void issue(const char *base, char *tile) const
+    {
+        char *t = tile + __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE) * TL::kPer * 1024;
+#pragma unroll
+        for (int i = 0; i < TL::kPer; ++i)
+            __builtin_amdgcn_global_load_lds(base + off[i], (lds_bytes *)(t + i * 1024), 16, 0, 0);
+    }
+};
+
+// The keys' side: 64 of K and V a step ahead.
+template <int DH> struct KeyStage {
+    Dma<DH> k, v;
+    uint32_t byte;                                     // the lane's key's mask byte
+
+    __device__ __forceinline__ explicit KeyStage(const AttnArgs &a)
+    {
+        k.rows(kManyStep - 1, (uint32_t)(a.ld_k * 2), a.D);
+        v.rows(kManyStep - 1, (uint32_t)(a.ld_v * 2), a.D);
+    }
+    __device__ __forceinline__ void issue(const AttnArgs &a, int h, int k0, int kb, int hi, char *kt, char *vt)
+    {
+        const int last = hi - 1 - kb;
+        if (last < kManyStep - 1) {
+            k.rows(last, (uint32_t)(a.ld_k * 2), a.D);
+            v.rows(last, (uint32_t)(a.ld_v * 2), a.D);
         }
+        byte = a.mask ? a.mask[k0 + kb + min(ams_lane(), last)] : 1;
+        k.issue((const char *)a.k + ((int64_t)(k0 + kb) * a.ld_k + (int64_t)h * a.D) * 2, kt);
+        v.issue((const char *)a.v + ((int64_t)(k0 + kb) * a.ld_v + (int64_t)h * a.D) * 2, vt);
+    }
+    // The tile of the keys from kb on is there: which of them take part.  Masked ones become zeros.
+    __device__ __forceinline__ uint64_t arrive(const AttnArgs &a, int kb, int hi, char *kt, char *vt)
+    {
+        staged();
+        const uint64_t kept = ams_ballot(byte != 0);
+        if (a.mask && kept != ~0ull) {
+            for (int i = threadIdx.x; i < kManyStep * Tile<DH>::kPieces; i += kAttnThreads) {
+                if (kept >> (i / Tile<DH>::kPieces) & 1) continue;
+                *(uint4 *)(kt + i * 16) = make_uint4(0, 0, 0, 0);
+                *(uint4 *)(vt + i * 16) = make_uint4(0, 0, 0, 0);
+            }
+            __syncthreads();
+        }
+        return kept & ams_ballot(kb + ams_lane() < hi);
+    }
+};
+
+// The rows' side: 64 of Q and dO a step ahead, with their log-sum-exp and delta.
+template <int DH> struct RowStage {
+    Dma<DH> q, d;
+    float lse, delta;
+    bool same = false;                                 // the offsets of a whole step hold for the next one
+
+    __device__ __forceinline__ void issue(const AttnArgs &a, int h, int q0, int rb, int hi, char *qt, char *dt)
+    {
+        // the step's first query; a row lies at most 64 queries on
+        const int qb = __builtin_amdgcn_readfirstlane(a.by_g.div(rb));
+        const int64_t query = (int64_t)q0 + qb;
+        const bool whole = rb + kManyStep <= hi;
+        if (!same || !whole) {
+#pragma unroll
+            for (int i = 0; i < Tile<DH>::kPer; ++i) {
+                const int r = min(rb + Dma<DH>::row(i), hi - 1), n = a.by_g.div(r);
+                const uint32_t col = (uint32_t)((r - n * a.G) * a.D * 2) + Dma<DH>::col(i, a.D);
+                q.off[i] = (uint32_t)(n - qb) * (uint32_t)(a.ld_q * 2) + col;
+                d.off[i] = (uint32_t)(n - qb) * (uint32_t)(a.ld_dout * 2) + col;
+            }
+            same = whole && kKeyTile % a.G == 0;       // steps begin on whole queries
+        }
+        const int r = min(rb + ams_lane(), hi - 1), n = a.by_g.div(r);
+        const int64_t at = ((int64_t)q0 + n) * a.H + h * a.G + (r - n * a.G);
+        lse = a.lse[at];
+        delta = a.delta[at];
+        q.issue((const char *)a.q + (query * a.ld_q + (int64_t)h * a.G * a.D) * 2, qt);
+        d.issue((const char *)a.dout + (query * a.ld_dout + (int64_t)h * a.G * a.D) * 2, dt);
     }
 };
 
@@ -163,7 +240,8 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_ma
 {
     using TL = Tile<DH>;
     constexpr int NC = DH / 16, ND = DH / 32;
-    __shared__ __attribute__((aligned(16))) char s_k[2][TL::kBytes], s_v[2][TL::kBytes];
+    // each buffer an array of its own, so that the compiler sees that a step's loads go elsewhere than its reads
+    __shared__ __attribute__((aligned(16))) char s_k0[TL::kBytes], s_k1[TL::kBytes], s_v0[TL::kBytes], s_v1[TL::kBytes];
     const int lane = ams_lane(), hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);
     const Work wk = many_work(xcd_block(), a);
@@ -191,18 +269,10 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_ma
 #pragma unroll
     for (int d = 0; d < ND; ++d) acc[d] = zero16();
     float mx = kNegInf, l = 0.f;
-    KeyStage<DH> st;
-    if (lo < hi) {
-        st.load(a, h, k0, lo, hi);
-        st.store(a, s_k[0], s_v[0]);
-    }
-    int buf = 0;
-    for (int kb = lo; kb < hi; kb += kManyStep, buf ^= 1) {
-        __syncthreads();                               // this tile is there, the other one free
-        const bool more = kb + kManyStep < hi;
-        const uint64_t live = st.live;
-        if (more) st.load(a, h, k0, kb + kManyStep, hi);
-        const char *kt = s_k[buf], *vt = s_v[buf];
+    KeyStage<DH> st(a);
+    auto step = [&](int kb, char *kt, char *vt, char *kn, char *vn) {
+        const uint64_t live = st.arrive(a, kb, hi, kt, vt);
+        if (kb + kManyStep < hi) st.issue(a, h, k0, kb + kManyStep, hi, kn, vn);
         f32x16 s[2] = {zero16(), zero16()};
 #pragma unroll
         for (int x = 0; x < NC; ++x)
@@ -245,7 +315,11 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_ma
 #pragma unroll
                 for (int d = 0; d < ND; ++d) acc[d] = mma32(TL::col_frag(vt, 32 * t + 16 * x, d), p, acc[d]);
             }
-        if (more) st.store(a, s_k[buf ^ 1], s_v[buf ^ 1]);
+    };
+    if (lo < hi) st.issue(a, h, k0, lo, hi, s_k0, s_v0);
+    for (int kb = lo; kb < hi; kb += 2 * kManyStep) {
+        step(kb, s_k0, s_v0, s_k1, s_v1);
+        if (kb + kManyStep < hi) step(kb + kManyStep, s_k1, s_v1, s_k0, s_v0);
     }
     l += __shfl_xor(l, 32, AMS_WAVE);
     if (r_mine >= R) return;
@@ -280,7 +354,8 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_man
 {
     using TL = Tile<DH>;
     constexpr int NC = DH / 16, ND = DH / 32;
-    __shared__ __attribute__((aligned(16))) char s_k[2][TL::kBytes], s_v[2][TL::kBytes];
+    // each buffer an array of its own, so that the compiler sees that a step's loads go elsewhere than its reads
+    __shared__ __attribute__((aligned(16))) char s_k0[TL::kBytes], s_k1[TL::kBytes], s_v0[TL::kBytes], s_v1[TL::kBytes];
     const int lane = ams_lane(), hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);
     const Work wk = many_work(xcd_block(), a);
@@ -320,18 +395,10 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_man
     f32x16 acc[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d) acc[d] = zero16();
-    KeyStage<DH> st;
-    if (lo < hi) {
-        st.load(a, h, k0, lo, hi);
-        st.store(a, s_k[0], s_v[0]);
-    }
-    int buf = 0;
-    for (int kb = lo; kb < hi; kb += kManyStep, buf ^= 1) {
-        __syncthreads();
-        const bool more = kb + kManyStep < hi;
-        const uint64_t live = st.live;
-        if (more) st.load(a, h, k0, kb + kManyStep, hi);
-        const char *kt = s_k[buf], *vt = s_v[buf];
+    KeyStage<DH> st(a);
+    auto step = [&](int kb, char *kt, char *vt, char *kn, char *vn) {
+        const uint64_t live = st.arrive(a, kb, hi, kt, vt);
+        if (kb + kManyStep < hi) st.issue(a, h, k0, kb + kManyStep, hi, kn, vn);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             f32x16 s = zero16(), dp = zero16();
@@ -343,7 +410,7 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_man
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const float p = __builtin_amdgcn_exp2f(s[r] * c - lse2);
-                s[r] = p * (dp[r] - delta) * a.scale;
+                s[r] = p * (dp[r] - delta);
             }
             if (live != ~0ull || all_on != ~0ull) {
 #pragma unroll
@@ -357,8 +424,14 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_man
                 for (int d = 0; d < ND; ++d) acc[d] = mma32(TL::col_frag(kt, 32 * t + 16 * x, d), p, acc[d]);
             }
         }
-        if (more) st.store(a, s_k[buf ^ 1], s_v[buf ^ 1]);
+    };
+    if (lo < hi) st.issue(a, h, k0, lo, hi, s_k0, s_v0);
+    for (int kb = lo; kb < hi; kb += 2 * kManyStep) {
+        step(kb, s_k0, s_v0, s_k1, s_v1);
+        if (kb + kManyStep < hi) step(kb + kManyStep, s_k1, s_v1, s_k0, s_v0);
     }
+#pragma unroll
+    for (int d = 0; d < ND; ++d) acc[d] *= a.scale;
     if (r_mine >= R) return;
     if (a.nsplit > 1) {
         float *p = a.part_o + ((int64_t)wk.split * a.n_q * a.H + at) * a.D;
@@ -385,7 +458,7 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads) void attn_dkv_many_
 {
     using TL = Tile<DH>;
     constexpr int NC = DH / 16, ND = DH / 32;
-    __shared__ __attribute__((aligned(16))) char s_q[2][TL::kBytes], s_d[2][TL::kBytes];
+    __shared__ __attribute__((aligned(16))) char s_q0[TL::kBytes], s_q1[TL::kBytes], s_d0[TL::kBytes], s_d1[TL::kBytes];
     __shared__ __attribute__((aligned(16))) float s_lse[2][kManyStep], s_delta[2][kManyStep];
     const int lane = ams_lane(), hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);
@@ -409,53 +482,21 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads) void attn_dkv_many_
 #pragma unroll
     for (int d = 0; d < ND; ++d) ak[d] = av[d] = zero16();
 
-    // rows a step ahead; a row that is not there or has no keys comes as zeros with a log-sum-exp of
-    // +infinity, so that its weights are zero
-    uint4 qr[TL::kPer], dr[TL::kPer];
-    float lr = 0.f, tr = 0.f;
-    bool there[TL::kPer];
-    auto load = [&](int rb) {
-#pragma unroll
-        for (int i = 0; i < TL::kPer; ++i) {
-            const int p = i * kAttnThreads + threadIdx.x, r = rb + p / TL::kPieces, piece = p % TL::kPieces;
-            const Row w = row_at(a, q0, h, r < hi ? r : hi - 1);
-            const int64_t col = (int64_t)w.head * a.D + (piece * 8 < a.D ? piece * 8 : 0);
-            qr[i] = *(const uint4 *)((const uint16_t *)a.q + w.query * a.ld_q + col);
-            dr[i] = *(const uint4 *)((const uint16_t *)a.dout + w.query * a.ld_dout + col);
-            there[i] = r < hi && piece * 8 < a.D && a.lse[w.query * a.H + w.head] != kNegInf;
-        }
-        if (threadIdx.x < kManyStep) {
-            const int r = rb + threadIdx.x;
-            const Row w = row_at(a, q0, h, r < hi ? r : hi - 1);
-            const float x = a.lse[w.query * a.H + w.head];
-            const bool ok = r < hi && x != kNegInf;
-            lr = ok ? x * kLog2e : -kNegInf;
-            tr = ok ? a.delta[w.query * a.H + w.head] : 0.f;
-        }
-    };
-    auto store = [&](int b) {
-#pragma unroll
-        for (int i = 0; i < TL::kPer; ++i) {
-            const int p = i * kAttnThreads + threadIdx.x, r = p / TL::kPieces, piece = p % TL::kPieces;
-            if (!there[i]) qr[i] = dr[i] = make_uint4(0, 0, 0, 0);
-            *(uint4 *)(s_q[b] + TL::at(r, piece)) = qr[i];
-            *(uint4 *)(s_d[b] + TL::at(r, piece)) = dr[i];
-        }
-        if (threadIdx.x < kManyStep) {
-            s_lse[b][threadIdx.x] = lr;
-            s_delta[b][threadIdx.x] = tr;
-        }
-    };
+    // rows a step ahead.  A row behind the last gets a log-sum-exp of +infinity, so that its weights are
+    // zero; all rows of a sample have the same keys, so one without any has no live key either and is left out.
     if (lo < hi) {
-        load(lo);
-        store(0);
+        const Row w = row_at(a, q0, h, 0);
+        const int bits = __builtin_amdgcn_readfirstlane((int)__float_as_uint(a.lse[w.query * a.H + w.head]));
+        if (__uint_as_float((uint32_t)bits) == kNegInf) hi = lo;
     }
-    int buf = 0;
-    for (int rb = lo; rb < hi; rb += kManyStep, buf ^= 1) {
-        __syncthreads();
-        const bool more = rb + kManyStep < hi;
-        if (more) load(rb + kManyStep);
-        const char *qt = s_q[buf], *dt = s_d[buf];
+    RowStage<DH> st;
+    auto step = [&](int rb, char *qt, char *dt, char *qn, char *dn, int buf) {
+        if (wave == 0) {
+            s_lse[buf][lane] = rb + lane < hi ? st.lse * kLog2e : -kNegInf;
+            s_delta[buf][lane] = st.delta;
+        }
+        staged();
+        if (rb + kManyStep < hi) st.issue(a, h, q0, rb + kManyStep, hi, qn, dn);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             f32x16 s = zero16(), dp = zero16();
@@ -472,7 +513,7 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads) void attn_dkv_many_
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     s[r + e] = __builtin_amdgcn_exp2f(s[r + e] * c - lv[e]);
-                    dp[r + e] = s[r + e] * (dp[r + e] - dv[e]) * a.scale;
+                    dp[r + e] = s[r + e] * (dp[r + e] - dv[e]);
                 }
             }
             if (all_live != ~0ull) {
@@ -492,8 +533,14 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads) void attn_dkv_many_
                 }
             }
         }
-        if (more) store(buf ^ 1);
+    };
+    if (lo < hi) st.issue(a, h, q0, lo, hi, s_q0, s_d0);
+    for (int rb = lo; rb < hi; rb += 2 * kManyStep) {
+        step(rb, s_q0, s_d0, s_q1, s_d1, 0);
+        if (rb + kManyStep < hi) step(rb + kManyStep, s_q1, s_d1, s_q0, s_d0, 1);
     }
+#pragma unroll
+    for (int d = 0; d < ND; ++d) ak[d] *= a.scale;
     if (mine >= keys.count) return;
     if (a.nsplit > 1) {
         float *p = a.part_o + ((int64_t)wk.split * a.n_k * a.Hk + key * a.Hk + h) * 2 * a.D;
