@@ -67,7 +67,12 @@ __device__ __forceinline__ int entry_of(int r, int hh) { return 8 * (r >> 2) + 4
 template <int DH> struct Tile {
     static constexpr int kPieces = DH / 8, kRowBytes = DH * 2, kBytes = kManyStep * kRowBytes,
                          kPer = kManyStep * kPieces / kAttnThreads;      // pieces a thread stages
-    __device__ static __forceinline__ int swizzle(int row) { return DH >= 64 ? row & 7 : (row >> 2) & 3; }
+    // A row read takes one piece of 16 consecutive rows at a time, a transposed read four pieces of 4 rows:
+    // with the row's low bits in the piece's high bits both fall on all 64 banks once.
+    __device__ static __forceinline__ int swizzle(int row)
+    {
+        return DH == 128 ? (row & 3) << 2 | (row >> 2 & 3) : (DH == 64 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : row >> 2 & 3);
+    }
     __device__ static __forceinline__ uint32_t at(int row, int piece)
     {
         return (uint32_t)(row * kRowBytes + ((piece ^ swizzle(row)) << 4));
