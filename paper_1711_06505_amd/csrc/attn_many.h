@@ -37,6 +37,16 @@ __device__ __forceinline__ void staged()
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// Two waves share a SIMD, one of either block on the compute unit.  Treated
+// alike they fall into step, both in their products and then both in their
+// exponentials; with one of them (by its slot) always first, the other one
+// fills in what it leaves free (364 and 512 us without, 353 and 495 with, forward
+// and dQ of 8 x 1536 queries, 16 heads of 128, 3072 keys).
+__device__ __forceinline__ void take_turns()
+{
+    if (__builtin_amdgcn_s_getreg((3 << 11) | 4) & 1) __builtin_amdgcn_s_setprio(1);
+}
+
 constexpr int kManyRows = 128;        // rows (keys) of a block, 32 a wave
 constexpr int kManyShift = 7;
 constexpr int kManyStep = 64;         // streamed entries of a tile
@@ -63,10 +73,10 @@ __device__ __forceinline__ Frag pack16(const f32x16 &x, int c)
 // entry of register r in lane half hh
 __device__ __forceinline__ int entry_of(int r, int hh) { return 8 * (r >> 2) + 4 * hh + (r & 3); }
 
-// A tile of 64 rows of DH bf16 values in shared memory.
-template <int DH> struct Tile {
-    static constexpr int kPieces = DH / 8, kRowBytes = DH * 2, kBytes = kManyStep * kRowBytes,
-                         kPer = kManyStep * kPieces / kAttnThreads;      // pieces a thread stages
+// A tile of N rows of DH bf16 values in shared memory.
+template <int DH, int N = kManyStep> struct Tile {
+    static constexpr int kRows = N, kPieces = DH / 8, kRowBytes = DH * 2, kBytes = N * kRowBytes,
+                         kPer = N * kPieces / kAttnThreads;              // pieces a thread stages
     // A row read takes one piece of 16 consecutive rows at a time, a transposed read four pieces of 4 rows:
     // with the row's low bits in the piece's high bits both fall on all 64 banks once.
     __device__ static __forceinline__ int swizzle(int row)
@@ -122,8 +132,8 @@ __device__ __forceinline__ Work many_work(int64_t b, const AttnArgs &a)
 // What lies behind D or behind the last row reads another piece of the tile:
 // the first meets zeros of the other operand or results that nobody stores,
 // the second weights of zero.
-template <int DH> struct Dma {
-    using TL = Tile<DH>;
+template <int DH, int N = kManyStep> struct Dma {
+    using TL = Tile<DH, N>;
     uint32_t off[TL::kPer];
 
     __device__ static __forceinline__ int slot(int i)
@@ -149,6 +159,19 @@ template <int DH> struct Dma {
             __builtin_amdgcn_global_load_lds(base + off[i], (lds_bytes *)(t + i * 1024), 16, 0, 0);
     }
 };
+
+// A list's rows into a tile that stays, with zeros behind D; there after the next barrier.
+template <int DH, int N>
+__device__ __forceinline__ void stage_rows(const char *base, int last, uint32_t ld, int D, char *tile)
+{
+    Dma<DH, N> dma;
+    dma.rows(last, ld, D);
+    dma.issue(base, tile);
+    if (D == DH) return;
+    staged();
+    for (int i = threadIdx.x; i < N * (DH / 8); i += kAttnThreads)
+        if (i % (DH / 8) * 8 >= D) *(uint4 *)(tile + Tile<DH, N>::at(i / (DH / 8), i % (DH / 8))) = make_uint4(0, 0, 0, 0);
+}
 
 // The keys' side: 64 of K and V a step ahead.
 template <int DH> struct KeyStage {
@@ -188,29 +211,30 @@ template <int DH> struct KeyStage {
     }
 };
 
-// The rows' side: 64 of Q and dO a step ahead, with their log-sum-exp and delta.
-template <int DH> struct RowStage {
-    Dma<DH> q, d;
+// The rows' side: N of Q and dO a step ahead, with their log-sum-exp and delta.
+template <int DH, int N> struct RowStage {
+    using DM = Dma<DH, N>;
+    DM q, d;
     float lse, delta;
     bool same = false;                                 // the offsets of a whole step hold for the next one
 
     __device__ __forceinline__ void issue(const AttnArgs &a, int h, int q0, int rb, int hi, char *qt, char *dt)
     {
-        // the step's first query; a row lies at most 64 queries on
+        // the step's first query; a row lies at most N queries on
         const int qb = __builtin_amdgcn_readfirstlane(a.by_g.div(rb));
         const int64_t query = (int64_t)q0 + qb;
-        const bool whole = rb + kManyStep <= hi;
+        const bool whole = rb + N <= hi;
         if (!same || !whole) {
 #pragma unroll
-            for (int i = 0; i < Tile<DH>::kPer; ++i) {
-                const int r = min(rb + Dma<DH>::row(i), hi - 1), n = a.by_g.div(r);
-                const uint32_t col = (uint32_t)((r - n * a.G) * a.D * 2) + Dma<DH>::col(i, a.D);
+            for (int i = 0; i < Tile<DH, N>::kPer; ++i) {
+                const int r = min(rb + DM::row(i), hi - 1), n = a.by_g.div(r);
+                const uint32_t col = (uint32_t)((r - n * a.G) * a.D * 2) + DM::col(i, a.D);
                 q.off[i] = (uint32_t)(n - qb) * (uint32_t)(a.ld_q * 2) + col;
                 d.off[i] = (uint32_t)(n - qb) * (uint32_t)(a.ld_dout * 2) + col;
             }
             same = whole && kKeyTile % a.G == 0;       // steps begin on whole queries
         }
-        const int r = min(rb + ams_lane(), hi - 1), n = a.by_g.div(r);
+        const int r = min(rb + (ams_lane() & (N - 1)), hi - 1), n = a.by_g.div(r);
         const int64_t at = ((int64_t)q0 + n) * a.H + h * a.G + (r - n * a.G);
         lse = a.lse[at];
         delta = a.delta[at];
@@ -274,6 +298,7 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_ma
 #pragma unroll
     for (int d = 0; d < ND; ++d) acc[d] = zero16();
     float mx = kNegInf, l = 0.f;
+    take_turns();
     KeyStage<DH> st(a);
     auto step = [&](int kb, char *kt, char *vt, char *kn, char *vn) {
         const uint64_t live = st.arrive(a, kb, hi, kt, vt);
@@ -400,6 +425,7 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_man
     f32x16 acc[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d) acc[d] = zero16();
+    take_turns();
     KeyStage<DH> st(a);
     auto step = [&](int kb, char *kt, char *vt, char *kn, char *vn) {
         const uint64_t live = st.arrive(a, kb, hi, kt, vt);
@@ -457,14 +483,20 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_man
 
 // ----------------------------------------------------------------- dK, dV
 
-// 128 keys a block, 32 a wave in registers; rows in tiles of 64 with their
-// log-sum-exp and delta.
-template <int DH> __global__ __launch_bounds__(kAttnThreads) void attn_dkv_many_k(AttnArgs a)
+// 128 keys a block, 32 a wave; rows in tiles with their log-sum-exp and delta.
+// Both sums of a wave are 2 DH registers.  For two waves per SIMD at DH = 128
+// the values stay in shared memory, read anew for each tile, and a tile is 32
+// rows (8 x 1536 queries, 16 heads, 3072 keys: 867 us; one wave per SIMD with all in registers: 1125).
+template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_many_k(AttnArgs a)
 {
-    using TL = Tile<DH>;
+    constexpr bool kShared = DH == 128;
+    constexpr int N = kShared ? 32 : 64;
+    using TL = Tile<DH, N>;
+    using VT = Tile<DH, kManyRows>;
     constexpr int NC = DH / 16, ND = DH / 32;
     __shared__ __attribute__((aligned(16))) char s_q0[TL::kBytes], s_q1[TL::kBytes], s_d0[TL::kBytes], s_d1[TL::kBytes];
-    __shared__ __attribute__((aligned(16))) float s_lse[2][kManyStep], s_delta[2][kManyStep];
+    __shared__ __attribute__((aligned(16))) char s_v[kShared ? VT::kBytes : 16];
+    __shared__ __attribute__((aligned(16))) float s_lse[2][N], s_delta[2][N];
     const int lane = ams_lane(), hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);
     const Work wk = many_work(xcd_block(), a);
@@ -479,9 +511,15 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads) void attn_dkv_many_
     const bool live_key = mine < keys.count && !(a.mask && a.mask[key] == 0);
     const uint64_t all_live = ams_ballot(live_key);
 
-    Frag kf[NC], vf[NC];
+    Frag kf[NC], vf[kShared ? 1 : NC];
     rows_frag<DH>(kf, a.k, a.ld_k, Row{key, h}, a.D);
-    rows_frag<DH>(vf, a.v, a.ld_v, Row{key, h}, a.D);
+    if constexpr (kShared) {
+        const char *vp = (const char *)a.v + ((keys.begin + keys.first) * a.ld_v + (int64_t)h * a.D) * 2;
+        const int64_t left = keys.count - 1 - keys.first;
+        stage_rows<DH, kManyRows>(vp, (int)(left < kManyRows - 1 ? left : kManyRows - 1), (uint32_t)(a.ld_v * 2), a.D, s_v);
+    } else {
+        rows_frag<DH>(vf, a.v, a.ld_v, Row{key, h}, a.D);
+    }
     const float c = a.scale * kLog2e;
     f32x16 ak[ND], av[ND];
 #pragma unroll
@@ -494,21 +532,23 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads) void attn_dkv_many_
         const int bits = __builtin_amdgcn_readfirstlane((int)__float_as_uint(a.lse[w.query * a.H + w.head]));
         if (__uint_as_float((uint32_t)bits) == kNegInf) hi = lo;
     }
-    RowStage<DH> st;
+    RowStage<DH, N> st;
+    take_turns();
     auto step = [&](int rb, char *qt, char *dt, char *qn, char *dn, int buf) {
-        if (wave == 0) {
+        if (wave == 0 && lane < N) {
             s_lse[buf][lane] = rb + lane < hi ? st.lse * kLog2e : -kNegInf;
             s_delta[buf][lane] = st.delta;
         }
         staged();
-        if (rb + kManyStep < hi) st.issue(a, h, q0, rb + kManyStep, hi, qn, dn);
+        if (rb + N < hi) st.issue(a, h, q0, rb + N, hi, qn, dn);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < N / 32; ++t) {
             f32x16 s = zero16(), dp = zero16();
 #pragma unroll
             for (int x = 0; x < NC; ++x) {
                 s = mma32(TL::row_frag(qt, 32 * t, x), kf[x], s);
-                dp = mma32(TL::row_frag(dt, 32 * t, x), vf[x], dp);
+                if constexpr (kShared) dp = mma32(TL::row_frag(dt, 32 * t, x), VT::row_frag(s_v, 32 * wave, x), dp);
+                else dp = mma32(TL::row_frag(dt, 32 * t, x), vf[x], dp);
             }
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
@@ -540,9 +580,9 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads) void attn_dkv_many_
         }
     };
     if (lo < hi) st.issue(a, h, q0, lo, hi, s_q0, s_d0);
-    for (int rb = lo; rb < hi; rb += 2 * kManyStep) {
+    for (int rb = lo; rb < hi; rb += 2 * N) {
         step(rb, s_q0, s_d0, s_q1, s_d1, 0);
-        if (rb + kManyStep < hi) step(rb + kManyStep, s_q1, s_d1, s_q0, s_d0, 1);
+        if (rb + N < hi) step(rb + N, s_q1, s_d1, s_q0, s_d0, 1);
     }
 #pragma unroll
     for (int d = 0; d < ND; ++d) ak[d] *= a.scale;
