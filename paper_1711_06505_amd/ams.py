@@ -425,44 +425,49 @@ class _Call:
     """Checks of one call's tensors (ValueError), then the call itself on the
     tensors' device and the given or current stream there."""
 
-    def __init__(self, where: str):
-        self.where, self.device = where, None
+    __slots__ = ("where", "device")
 
-    def _same_device(self, name, t):
-        if t.device.type != "cuda":
+    def __init__(self, where: str, first):
+        """All of the call's tensors have to be on the device of `first`, a GPU."""
+        self.where = where
+        self.device = first.get_device() if first.is_cuda else -2      # no tensor's
+
+    def _refuse(self, name, t, dtype, need):
+        if t.dtype != dtype:
+            raise ValueError(f"{self.where}: {name} must be {dtype}, not {t.dtype}")
+        if need:
+            raise ValueError(f"{self.where}: {need}")
+        if not t.is_cuda:
             raise ValueError(f"{self.where}: {name} is on {t.device}, not on a GPU")
-        if self.device is None:
-            self.device = t.device
-        elif t.device != self.device:
-            raise ValueError(f"{self.where}: {name} is on {t.device}, other arguments on {self.device}")
+        raise ValueError(f"{self.where}: {name} is on {t.device}, other arguments are not")
 
     def vec(self, name, t, dtype, least: int):
-        """A contiguous tensor of at least `least` elements."""
-        if t.dtype != dtype:
-            raise ValueError(f"{self.where}: {name} must be {dtype}, not {t.dtype}")
-        if not t.is_contiguous():
-            raise ValueError(f"{self.where}: {name} must be contiguous")
-        if t.numel() < least:
-            raise ValueError(f"{self.where}: {name} has {t.numel()} elements, {least} needed")
-        self._same_device(name, t)
-        return _p(t)
+        """Address of a contiguous tensor of at least `least` elements."""
+        if t.dtype != dtype or not t.is_contiguous() or t.numel() < least or t.get_device() != self.device:
+            self._refuse(name, t, dtype, f"{name} must be contiguous" if not t.is_contiguous() else
+                         f"{name} has {t.numel()} elements, {least} needed" if t.numel() < least else None)
+        return t.data_ptr()
 
     def rows(self, name, t, dtype, n: int, inner):
-        """Rows of `inner` (contiguous within a row), at least n of them;
-        returns (pointer, row stride)."""
-        if t.dtype != dtype:
-            raise ValueError(f"{self.where}: {name} must be {dtype}, not {t.dtype}")
-        if tuple(t.shape[1:]) != tuple(inner) or t.shape[0] < n:
-            raise ValueError(f"{self.where}: {name} is {tuple(t.shape)}, [{n}, {', '.join(map(str, inner))}] needed")
-        width = 1
-        for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-            if size > 1 and stride != width:
-                raise ValueError(f"{self.where}: a row of {name} must be contiguous")
-            width *= size
-        if t.shape[0] > 1 and t.stride(0) < width:
-            raise ValueError(f"{self.where}: the rows of {name} overlap")
-        self._same_device(name, t)
-        return _p(t), max(t.stride(0), width) if t.shape[0] > 1 else width
+        """Rows of `inner` (contiguous within a row), at least n of them:
+        (address, row stride)."""
+        shape = t.shape
+        if t.dtype != dtype or shape[1:] != inner or shape[0] < n:
+            self._refuse(name, t, dtype, f"{name} is {tuple(shape)}, [{n}, {', '.join(map(str, inner))}] needed")
+        ld = width = inner[0] if len(inner) == 1 else inner[0] * inner[1]
+        if not t.is_contiguous():
+            w = 1
+            for size, stride in zip(reversed(inner), reversed(t.stride()[1:])):
+                if size > 1 and stride != w:
+                    self._refuse(name, t, dtype, f"a row of {name} must be contiguous")
+                w *= size
+            if shape[0] > 1:
+                ld = t.stride(0)
+                if ld < width:
+                    self._refuse(name, t, dtype, f"the rows of {name} overlap")
+        if t.get_device() != self.device:
+            self._refuse(name, t, dtype, None)
+        return t.data_ptr(), ld
 
     def storage(self, name, t) -> int:
         if t.dtype not in _STORAGE:
@@ -477,19 +482,20 @@ class _Call:
     def run(self, f, *args, stream=None):
         if stream is None:
             stream = torch.cuda.current_stream(self.device)
-        elif stream.device != self.device:
-            raise ValueError(f"{self.where}: a stream of {stream.device}, tensors on {self.device}")
-        if self.device.index == torch.cuda.current_device():
-            rc = f(*args, ctypes.c_void_p(stream.cuda_stream))
+        elif stream.device.index != self.device:
+            raise ValueError(f"{self.where}: a stream of {stream.device}, tensors on cuda:{self.device}")
+        if self.device == torch.cuda.current_device():
+            rc = f(*args, stream.cuda_stream)
         else:
             with torch.cuda.device(self.device):
-                rc = f(*args, ctypes.c_void_p(stream.cuda_stream))
-        _check(rc, self.where)
+                rc = f(*args, stream.cuda_stream)
+        if rc:
+            raise AmsError(rc, self.where)
 
 
 def ams_lookup_fwd(ids, table, out, scale: float = 1.0, pad_id: int = -1, stream=None):
     """out[k] = scale * table[ids[k]] (float32 or bfloat16 rows, any row stride)."""
-    c = _Call("ams_lookup_fwd")
+    c = _Call("ams_lookup_fwd", ids)
     n, D = ids.numel(), table.shape[1]
     dt = c.storage("table", table)
     ip = c.vec("ids", ids, torch.int32, n)
@@ -507,7 +513,7 @@ def ams_lookup_bwd(uniq, inv, occ_perm, uniq_off, n_uniq, n_uniq_cap: int, dout,
                    pad_id: int = -1, stream=None):
     """grad[u] = scale * the sum of dout over the tokens of uniq[u], from the
     outputs of ams_dedup over the tokens' IDs (dout has one row per token)."""
-    c = _Call("ams_lookup_bwd")
+    c = _Call("ams_lookup_bwd", dout)
     n, D = dout.shape
     dt, i32 = c.storage("dout", dout), torch.int32
     dp, ldd = c.rows("dout", dout, dout.dtype, n, (D,))
@@ -546,7 +552,7 @@ def _xattn_inputs(c, attn, q_off, k_off, q, k, v, key_mask):
 def ams_xattn_fwd(attn: ams_attn, q_off, k_off, q, k, v, out, lse, ws, key_mask=None, stream=None):
     """Attention of each sample's queries q [n_q, heads, dim] to its keys k, v
     [n_k, kv_heads, dim]; lse [n_q, heads] (None: not stored)."""
-    c = _Call("ams_xattn_fwd")
+    c = _Call("ams_xattn_fwd", q)
     lists, arrays = _xattn_inputs(c, attn, q_off, k_off, q, k, v, key_mask)
     n_q, T = q.shape[0], q.dtype
     o = c.rows("out", out, T, n_q, (attn.n_heads, attn.head_dim))
@@ -558,7 +564,7 @@ def ams_xattn_fwd(attn: ams_attn, q_off, k_off, q, k, v, out, lse, ws, key_mask=
 def ams_xattn_bwd(attn: ams_attn, q_off, k_off, q, k, v, out, lse, dout, dq, dk, dv, ws, key_mask=None, stream=None):
     """Gradients dq, dk, dv (overwritten) of ams_xattn_fwd's inputs, from its
     out and lse and the upstream gradient dout."""
-    c = _Call("ams_xattn_bwd")
+    c = _Call("ams_xattn_bwd", q)
     lists, arrays = _xattn_inputs(c, attn, q_off, k_off, q, k, v, key_mask)
     n_q, n_k, T = q.shape[0], k.shape[0], q.dtype
     hq, hk = (attn.n_heads, attn.head_dim), (attn.n_kv_heads, attn.head_dim)
@@ -588,7 +594,7 @@ def ams_cache_write(cache: ams_cache, new_off, start, page_table, k, v, k_codes,
     """Appends new tokens' keys and values k, v [n_new, kv_heads, dim] behind
     each sample's start[i] tokens; codes [n_pages, kv_heads, page, dim] uint8
     and scales [n_pages, kv_heads]."""
-    c = _Call("ams_cache_write")
+    c = _Call("ams_cache_write", k)
     B, n, i32 = new_off.numel() - 1, k.shape[0], torch.int32
     inner = (cache.n_kv_heads, cache.head_dim)
     dt = c.storage("k", k)
@@ -609,7 +615,7 @@ def ams_cache_attn(attn: ams_attn, cache: ams_cache, q_off, lengths, page_table,
                    out, ws, lse=None, stream=None):
     """Attention of each sample's queries q [n_q, heads, dim] to the first
     lengths[i] tokens that its pages hold."""
-    c = _Call("ams_cache_attn")
+    c = _Call("ams_cache_attn", q)
     B, n_q, i32, T = q_off.numel() - 1, q.shape[0], torch.int32, c.storage_of(attn)
     if (attn.n_kv_heads, attn.head_dim) != (cache.n_kv_heads, cache.head_dim):
         raise AmsError(4, c.where)

@@ -69,8 +69,8 @@ def test_binding_refusals():
     with pytest.raises(ams.AmsError, match="DIMS"):
         ams.ams_cache_attn(ams.make_attn(4, 2, 12, "f32"), cache, off, start, table, torch.zeros((1, 4, 12)), *pool,
                            torch.zeros((1, 4, 12)), torch.zeros(1, dtype=torch.uint8))
-    c = ams._Call("x")
-    c._same_device = lambda name, t: None
+    c = ams._Call("x", k)
+    c.device = -1                       # the tensors'
     with pytest.raises(ValueError, match="elements"):
         ams._cache_arrays(c, cache, 1, table, codes[:3], scale, codes, scale)
     with pytest.raises(ValueError, match="page_table has"):

@@ -59,8 +59,8 @@ def test_binding_refusals():
         with pytest.raises(ValueError, match=text):
             if change:     # these are seen before the device is asked for
                 args = {**ok, **change}
-                c = ams._Call("ams_xattn_fwd")
-                c._same_device = lambda name, t: None
+                c = ams._Call("ams_xattn_fwd", q)
+                c.device = -1                   # the tensors'
                 ams._xattn_inputs(c, attn, args["q_off"], args["k_off"], args["q"], args["k"], args["v"],
                                   args.get("key_mask"))
                 c.rows("out", args["out"], q.dtype, 2, (4, 16))
