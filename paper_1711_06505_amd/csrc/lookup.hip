@@ -102,12 +102,13 @@ __global__ __launch_bounds__(kThreads) void lookup_bwd_k(int D, int nv, int roun
                                                          float *__restrict__ grad, float *__restrict__ part)
 {
     constexpr int G = AMS_WAVE / L;
-    const int lane = ams_lane(), g = lane / L;
-    const int c = blockIdx.y * L + lane % L;
+    const int lane = ams_lane(), g = lane / L, wave = threadIdx.x / AMS_WAVE;
+    // rows wider than a wave's 64 pieces: the block's waves take neighbouring column tiles of one chunk
+    const int c = (L == AMS_WAVE ? blockIdx.y * kWaves + wave : blockIdx.y) * L + lane % L;
     const bool col = c < nv;
-    const int64_t chunk = (int64_t)blockIdx.x * kWaves + threadIdx.x / AMS_WAVE;
+    const int64_t chunk = L == AMS_WAVE ? blockIdx.x : (int64_t)blockIdx.x * kWaves + wave;
     const int64_t p0 = chunk * rounds * AMS_WAVE;
-    if (p0 >= n) return;
+    if (p0 >= n || (L == AMS_WAVE && c - lane >= nv)) return;
 
     auto row_of = [&](int64_t p, int &k) -> int {      // unique row of a sorted position (-1: none), and its token
         k = -1;
@@ -421,7 +422,8 @@ extern "C" ams_status ams_lookup_bwd(int32_t dtype, int32_t D, float scale, int3
         return with_lanes(L, [&](auto nl) {
             constexpr int NP = decltype(np)::value, NL = decltype(nl)::value;
             const unsigned tiles = (unsigned)((nv + NL - 1) / NL);
-            const dim3 g1((unsigned)((chunks + kWaves - 1) / kWaves), tiles);
+            const dim3 g1 = NL == AMS_WAVE ? dim3((unsigned)chunks, (tiles + kWaves - 1) / kWaves)
+                                           : dim3((unsigned)((chunks + kWaves - 1) / kWaves), tiles);
             AMS_LAUNCH("lookup_bwd", st,
                        lookup_bwd_k<T, NP, NL><<<g1, kThreads, 0, st>>>(D, nv, rounds, scale, pad_id, n, uniq, inv,
                                                                        occ_perm, n_uniq_cap, (const T *)dout, ld_dout,
