@@ -323,7 +323,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dkv_k(AttnArgs a)
 // contract over rows); a key tile's dK and dV are complete at once.  One more
 // block looks whether a sample has more rows than that.
 template <class T, int DH, int PB, int RT>
-__global__ __launch_bounds__(kAttnThreads, (waves_per_simd<T, DH, RT>())) void attn_bwd_few_k(AttnArgs a)
+__global__ __launch_bounds__(kAttnThreads, (DH == 128 ? 1 : waves_per_simd<T, DH, RT>())) void attn_bwd_few_k(AttnArgs a)
 {
     if (blockIdx.x == gridDim.x - 1) {
         bool found = false;
@@ -555,9 +555,6 @@ __global__ __launch_bounds__(kAttnThreads) void attn_sum_k(const float *part, in
 
 // ------------------------------------------------------------------- host
 
-// Rows of a sample, on average, from which the 32-row kernels are the faster ones.
-constexpr int64_t kManyFrom = 64;
-
 struct Plan {
     Cut fwd, dq;
     bool many;                        // the kernels of attn_many.h
@@ -567,6 +564,15 @@ struct Plan {
     size_t delta, total;              // workspace: delta's bytes, all
 };
 
+// A block of attn_many.h has 128 rows of partial sums to write and join again: a split per compute unit, of 512
+// entries at least.
+int split_many(int64_t tiles, int64_t entries)
+{
+    if (tiles < 1) tiles = 1;
+    const int64_t n = 256 / tiles < entries / 512 ? 256 / tiles : entries / 512;
+    return n < 1 ? 1 : (int)n;
+}
+
 ams_status plan_of(const ams_attn *at, int32_t B, int64_t n_q, int64_t n_k, bool wide, Plan &p)
 {
     const ams_status s = attn_shape(at);
@@ -575,11 +581,14 @@ ams_status plan_of(const ams_attn *at, int32_t B, int64_t n_q, int64_t n_k, bool
     if (B < 0 || n_q < 0 || n_k < 0 || n_q * G > INT32_MAX || n_k > INT32_MAX) return AMS_ERR_SIZE;
     const int64_t samples = B < 1 ? 1 : B, rows = n_q * G, keys = n_k / samples;
     p.fwd = p.dq = cut_rows(at, B, n_q, keys, wide);
-    p.many = wide && at->dtype == AMS_BF16 && rows >= kManyFrom * samples;
+    // 32-row products through shared memory once the rows of a sample are more than attn_bwd_few_k's tile on
+    // average (512 samples of 200 keys, 4 heads of 64, forward + backward: 35 + 48 us at 32 rows against 39 + 136
+    // with those, 48 + 176 at 48 rows against 42 + 119)
+    p.many = wide && at->dtype == AMS_BF16 && rows > (at->head_dim <= 64 ? 32 : 16) * samples;
     if (p.many) {
         int64_t busy = (rows + kManyRows - 1) >> kManyShift;
         if (busy < samples) busy = samples;
-        p.fwd.nsplit = p.dq.nsplit = split_count(busy * Hk, keys);
+        p.fwd.nsplit = p.dq.nsplit = split_many(busy * Hk, keys);
         p.fwd.tiles = p.dq.tiles = tiles_of(rows, kManyShift, B);
         p.fwd.blocks = p.dq.blocks = p.fwd.tiles * Hk * p.fwd.nsplit;
     }
@@ -596,7 +605,8 @@ ams_status plan_of(const ams_attn *at, int32_t B, int64_t n_q, int64_t n_k, bool
     const int key_shift = p.many ? kManyShift : 6;
     p.key_tiles = tiles_of(n_k, key_shift, B);
     const int64_t kt = (n_k + (1 << key_shift) - 1) >> key_shift, ks = n_k < B ? n_k : B;
-    p.dkv = p.few_rows > 0 ? 1 : split_count((kt > ks ? kt : ks) * Hk, rows / samples);
+    const int64_t key_blocks = (kt > ks ? kt : ks) * Hk;
+    p.dkv = p.few_rows > 0 ? 1 : (p.many ? split_many : split_count)(key_blocks, rows / samples);
     if (p.fwd.blocks > kAttnMaxBlocks || p.dq.blocks > kAttnMaxBlocks || p.key_tiles * Hk * p.dkv > kAttnMaxBlocks)
         return AMS_ERR_SIZE;
     const size_t all = (size_t)n_q * at->n_heads, D = at->head_dim, f = sizeof(float);
