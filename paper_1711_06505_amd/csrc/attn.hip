@@ -501,8 +501,8 @@ __global__ __launch_bounds__(kAttnThreads, (DH == 128 ? 1 : waves_per_simd<T, DH
             f32x4 ak[VD], av[VD];
 #pragma unroll
             for (int e = 0; e < VD; ++e) ak[e] = av[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-            mma_slice<T, DH>(ak, qs, Stream<T>(ds));
-            mma_slice<T, DH>(av, os, Stream<T>(p));
+            mma_slice<T, DH, RT == 1>(ak, qs, Stream<T>(ds));
+            mma_slice<T, DH, RT == 1>(av, os, Stream<T>(p));
             const int key = kb + 16 * t + m;
             if (key < hi) {
                 float o[4 * VD];
@@ -564,15 +564,6 @@ struct Plan {
     size_t delta, total;              // workspace: delta's bytes, all
 };
 
-// A block of attn_many.h has 128 rows of partial sums to write and join again: a split per compute unit, of 512
-// entries at least.
-int split_many(int64_t tiles, int64_t entries)
-{
-    if (tiles < 1) tiles = 1;
-    const int64_t n = 256 / tiles < entries / 512 ? 256 / tiles : entries / 512;
-    return n < 1 ? 1 : (int)n;
-}
-
 ams_status plan_of(const ams_attn *at, int32_t B, int64_t n_q, int64_t n_k, bool wide, Plan &p)
 {
     const ams_status s = attn_shape(at);
@@ -581,17 +572,10 @@ ams_status plan_of(const ams_attn *at, int32_t B, int64_t n_q, int64_t n_k, bool
     if (B < 0 || n_q < 0 || n_k < 0 || n_q * G > INT32_MAX || n_k > INT32_MAX) return AMS_ERR_SIZE;
     const int64_t samples = B < 1 ? 1 : B, rows = n_q * G, keys = n_k / samples;
     p.fwd = p.dq = cut_rows(at, B, n_q, keys, wide);
-    // 32-row products through shared memory once the rows of a sample are more than attn_bwd_few_k's tile on
-    // average (512 samples of 200 keys, 4 heads of 64, forward + backward: 35 + 48 us at 32 rows against 39 + 136
-    // with those, 48 + 176 at 48 rows against 42 + 119)
-    p.many = wide && at->dtype == AMS_BF16 && rows > (at->head_dim <= 64 ? 32 : 16) * samples;
-    if (p.many) {
-        int64_t busy = (rows + kManyRows - 1) >> kManyShift;
-        if (busy < samples) busy = samples;
-        p.fwd.nsplit = p.dq.nsplit = split_many(busy * Hk, keys);
-        p.fwd.tiles = p.dq.tiles = tiles_of(rows, kManyShift, B);
-        p.fwd.blocks = p.dq.blocks = p.fwd.tiles * Hk * p.fwd.nsplit;
-    }
+    // from more rows than attn_bwd_few_k's tile holds (512 samples of 200 keys, 4 heads of 64, forward + backward:
+    // 35 + 48 us at 32 rows against 39 + 136 with attn_many.h, 48 + 176 at 48 rows against 42 + 119)
+    p.many = wide && at->dtype == AMS_BF16 && cut_many(at, B, n_q, keys, at->head_dim <= 64 ? 32 : 16, p.fwd);
+    if (p.many) p.dq = p.fwd;
     // one pass over the keys where most samples' rows fit one tile
     p.few_rt = wide && at->head_dim <= 64 && rows > 8 * samples ? 2 : 1;
     p.few_rows = rows <= 16 * p.few_rt * samples ? 16 * p.few_rt : -1;
@@ -676,7 +660,7 @@ extern "C" ams_status ams_xattn_fwd(const ams_attn *attn, int32_t B, const int32
         if constexpr (PB == 16 && sizeof(T) == 2) {
             if (pl.many) {
                 AMS_LAUNCH("xattn_fwd_many", st,
-                           attn_fwd_many_k<DH><<<(unsigned)pl.fwd.blocks, kAttnThreads, 0, st>>>(a));
+                           attn_fwd_many_k<DH, false><<<(unsigned)pl.fwd.blocks, kAttnThreads, 0, st>>>(a));
                 if (a.nsplit > 1) launch_join<T>("xattn_join", a, st);
                 return ams_launch_status();
             }

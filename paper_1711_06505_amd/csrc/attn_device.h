@@ -244,8 +244,9 @@ template <class T> struct Stream {
     }
 };
 
-// acc[t] += slice tile t times the stream, over all VD tiles.
-template <class T, int DH>
+// acc[t] += slice tile t times the stream, over all VD tiles.  HALF: the stream's
+// second 16 entries are zero (float has an instruction group for each half).
+template <class T, int DH, bool HALF = false>
 __device__ __forceinline__ void mma_slice(f32x4 *acc, const Slice<T, DH> &s, const Stream<T> &p)
 {
 #pragma unroll
@@ -253,7 +254,8 @@ __device__ __forceinline__ void mma_slice(f32x4 *acc, const Slice<T, DH> &s, con
         Frag f[Num<T>::SF];
         s.frags(t, f);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) acc[t] = mma<T>(f[sizeof(T) == 4 ? i : 0], p.f[i], acc[t]);
+        for (int i = 0; i < (HALF && sizeof(T) == 4 ? 1 : 2); ++i)
+            acc[t] = mma<T>(f[sizeof(T) == 4 ? i : 0], p.f[i], acc[t]);
     }
 }
 
@@ -469,7 +471,6 @@ __global__ __launch_bounds__(kAttnThreads, (waves_per_simd<T, DH, RT>())) void a
         const int64_t r = rows.first + 16 * t + m;
         row[t] = row_at(a, rows.begin, h, (int)(r < R ? r : R - 1));
         rc.load(qf[t], (const char *)a.q + (row[t].query * a.ld_q + (int64_t)row[t].head * a.D) * ES, 0);
-        rc.clean(qf[t]);
     }
     const float c = a.scale * kLog2e;
     f32x4 acc[RT][VD];
@@ -624,6 +625,8 @@ __global__ __launch_bounds__(kAttnThreads, (waves_per_simd<T, DH, RT>())) void a
         issue(now, kb, page);
         int next = kb + kStep < hi ? kb + kStep : kb;
         pages_of(next, page);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) rc.clean(qf[t]);      // waits for the queries, behind the first keys' loads
         for (;;) {
             issue(then, next, page);
             const int after = next + kStep < hi ? next + kStep : next;

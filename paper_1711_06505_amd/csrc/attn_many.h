@@ -211,6 +211,67 @@ template <int DH> struct KeyStage {
     }
 };
 
+// The same from 8-bit pages: codes a step ahead in registers, page numbers two;
+// decoded on the way into shared memory, once for all four waves.  Tokens that
+// take no part become zeros there.
+template <int DH> struct PageStage {
+    using TL = Tile<DH>;
+    static constexpr int kUnits = kManyStep * DH / 16, kPer = (kUnits + kAttnThreads - 1) / kAttnThreads;
+    uint4 k[kPer], v[kPer];
+    float ks, vs, ks_next, vs_next;                    // of the lane's token
+    int page;                                          // of the lane's token, a step ahead of the codes
+    bool there, there_next;
+
+    __device__ __forceinline__ explicit PageStage(const AttnArgs &) {}
+    __device__ __forceinline__ void find(const AttnArgs &a, const int32_t *pages, int kb, int hi)
+    {
+        page = pages[min(kb + ams_lane(), hi - 1) >> a.page_shift];
+    }
+    __device__ __forceinline__ void issue(const AttnArgs &a, int h, int kb, int hi)
+    {
+        there_next = page >= 0 && page < a.n_pages;
+        const int mine = there_next ? page : 0;
+        const int64_t at = (int64_t)mine * a.Hk + h;
+        ks_next = a.ks[at];
+        vs_next = a.vs[at];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int u = min(i * kAttnThreads + (int)threadIdx.x, kUnits - 1), row = u / (DH / 16), piece = u % (DH / 16);
+            const int tok = min(kb + row, hi - 1), p = __shfl(mine, min(row, hi - 1 - kb), AMS_WAVE);
+            const int64_t first = ((((int64_t)p * a.Hk + h) << a.page_shift) + (tok & ((1 << a.page_shift) - 1))) * a.D +
+                                  (piece * 16 < a.D ? piece * 16 : 0);
+            k[i] = *(const uint4 *)(a.kc + first);
+            v[i] = *(const uint4 *)(a.vc + first);
+        }
+    }
+    __device__ __forceinline__ uint64_t arrive(int kb, int hi, char *kt, char *vt)
+    {
+        there = there_next, ks = ks_next, vs = vs_next;
+        const uint64_t live = ams_ballot(there && kb + ams_lane() < hi);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int u = i * kAttnThreads + threadIdx.x, row = u / (DH / 16), piece = u % (DH / 16);
+            if (kUnits % kAttnThreads && u >= kUnits) break;
+            if (!(live >> row & 1)) k[i] = v[i] = make_uint4(0, 0, 0, 0);
+            uint32_t x[8];
+            auto put = [&](const uint4 &c, char *tile) {
+                decode4<uint16_t>(c.x, x), decode4<uint16_t>(c.y, x + 2), decode4<uint16_t>(c.z, x + 4), decode4<uint16_t>(c.w, x + 6);
+                *(uint4 *)(tile + TL::at(row, 2 * piece)) = make_uint4(x[0], x[1], x[2], x[3]);
+                *(uint4 *)(tile + TL::at(row, 2 * piece + 1)) = make_uint4(x[4], x[5], x[6], x[7]);
+            };
+            put(k[i], kt);
+            put(v[i], vt);
+        }
+        staged();
+        return live;
+    }
+    // scale of the 16 tokens from 16 g on (they share a page)
+    __device__ __forceinline__ static float of(float x, int g)
+    {
+        return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 16 * g));
+    }
+};
+
 // The rows' side: N of Q and dO a step ahead, with their log-sum-exp and delta.
 template <int DH, int N> struct RowStage {
     using DM = Dma<DH, N>;
@@ -265,7 +326,7 @@ __device__ __forceinline__ void store4(void *row, int d, int D, float a, float b
 
 // ---------------------------------------------------------------- forward
 
-template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_many_k(AttnArgs a)
+template <int DH, bool PAGED> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_many_k(AttnArgs a)
 {
     using TL = Tile<DH>;
     constexpr int NC = DH / 16, ND = DH / 32;
@@ -280,9 +341,18 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_ma
     if (rows.first < 0 || rows.first >= R) return;
     const int64_t r_mine = rows.first + wave * 32 + (lane & 31);
     const Row row = row_at(a, rows.begin, h, (int)(r_mine < R ? r_mine : R - 1));
-    const int k0 = clamp_off(a.k_off[rows.i], a.n_k), k1 = clamp_off(a.k_off[rows.i + 1], a.n_k);
+    int k0 = 0, nk;
+    const int32_t *pages = nullptr;
+    if constexpr (PAGED) {
+        nk = clamp_off(a.len[rows.i], (int64_t)a.max_pages << a.page_shift);
+        pages = a.page_table + (int64_t)rows.i * a.max_pages;
+    } else {
+        k0 = clamp_off(a.k_off[rows.i], a.n_k);
+        const int k1 = clamp_off(a.k_off[rows.i + 1], a.n_k);
+        nk = k1 > k0 ? k1 - k0 : 0;
+    }
     int lo, hi;
-    split_range(k1 > k0 ? k1 - k0 : 0, wk.split, a.nsplit, lo, hi);
+    split_range(nk, wk.split, a.nsplit, lo, hi);
 
     Frag qf[NC];
     rows_frag<DH>(qf, a.q, a.ld_q, row, a.D);
@@ -299,15 +369,31 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_ma
     for (int d = 0; d < ND; ++d) acc[d] = zero16();
     float mx = kNegInf, l = 0.f;
     take_turns();
-    KeyStage<DH> st(a);
+    typename std::conditional<PAGED, PageStage<DH>, KeyStage<DH>>::type st(a);
     auto step = [&](int kb, char *kt, char *vt, char *kn, char *vn) {
-        const uint64_t live = st.arrive(a, kb, hi, kt, vt);
-        if (kb + kManyStep < hi) st.issue(a, h, k0, kb + kManyStep, hi, kn, vn);
+        uint64_t live;
+        float sk[4] = {c, c, c, c}, sv[4] = {1.f, 1.f, 1.f, 1.f};
+        if constexpr (PAGED) {
+            live = st.arrive(kb, hi, kt, vt);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) sk[g] = c * st.of(st.ks, g), sv[g] = st.of(st.vs, g);
+            if (kb + kManyStep < hi) {
+                st.issue(a, h, kb + kManyStep, hi);
+                if (kb + 2 * kManyStep < hi) st.find(a, pages, kb + 2 * kManyStep, hi);
+            }
+        } else {
+            live = st.arrive(a, kb, hi, kt, vt);
+            if (kb + kManyStep < hi) st.issue(a, h, k0, kb + kManyStep, hi, kn, vn);
+        }
         f32x16 s[2] = {zero16(), zero16()};
 #pragma unroll
         for (int x = 0; x < NC; ++x)
 #pragma unroll
             for (int t = 0; t < 2; ++t) s[t] = mma32(TL::row_frag(kt, 32 * t, x), qf[x], s[t]);
+        if constexpr (PAGED) {                         // a page's scale: registers 8 g .. 8 g + 7 are 16 tokens
+#pragma unroll
+            for (int r = 0; r < 32; ++r) s[r >> 4][r & 15] *= sk[r >> 3];
+        }
         if (live != ~0ull) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -321,7 +407,7 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_ma
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) tm = fmaxf(tm, s[t][r]);
-        tm = fmaxf(tm, __shfl_xor(tm, 32, AMS_WAVE)) * c;
+        tm = fmaxf(tm, __shfl_xor(tm, 32, AMS_WAVE)) * (PAGED ? 1.f : c);
         if (ams_ballot(tm > mx + 8.f)) {
             const float mn = fmaxf(mx, tm), alpha = __builtin_amdgcn_exp2f(mx - (mn == kNegInf ? 0.f : mn));
             mx = mn;
@@ -334,8 +420,9 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_ma
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[t][r] = __builtin_amdgcn_exp2f(s[t][r] * c - base);
+                s[t][r] = __builtin_amdgcn_exp2f(PAGED ? s[t][r] - base : s[t][r] * c - base);
                 l += s[t][r];
+                if constexpr (PAGED) s[t][r] = s[t][r] == 0.f ? 0.f : s[t][r] * sv[2 * t + (r >> 3)];
             }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -346,7 +433,15 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_ma
                 for (int d = 0; d < ND; ++d) acc[d] = mma32(TL::col_frag(vt, 32 * t + 16 * x, d), p, acc[d]);
             }
     };
-    if (lo < hi) st.issue(a, h, k0, lo, hi, s_k0, s_v0);
+    if (lo < hi) {
+        if constexpr (PAGED) {
+            st.find(a, pages, lo, hi);
+            st.issue(a, h, lo, hi);
+            if (lo + kManyStep < hi) st.find(a, pages, lo + kManyStep, hi);
+        } else {
+            st.issue(a, h, k0, lo, hi, s_k0, s_v0);
+        }
+    }
     for (int kb = lo; kb < hi; kb += 2 * kManyStep) {
         step(kb, s_k0, s_v0, s_k1, s_v1);
         if (kb + kManyStep < hi) step(kb + kManyStep, s_k1, s_v1, s_k0, s_v0);
@@ -606,6 +701,31 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_ma
             store4(dk, 32 * d + entry_of(r, hh), a.D, ak[d][r], ak[d][r + 1], ak[d][r + 2], ak[d][r + 3]);
             store4(dv, 32 * d + entry_of(r, hh), a.D, av[d][r], av[d][r + 1], av[d][r + 2], av[d][r + 3]);
         }
+}
+
+// ------------------------------------------------------------------- host
+
+// A block of attn_many.h has 128 rows of partial sums to write and join again: a split per compute unit, of 512
+// entries at least.
+inline int split_many(int64_t tiles, int64_t entries)
+{
+    if (tiles < 1) tiles = 1;
+    const int64_t n = 256 / tiles < entries / 512 ? 256 / tiles : entries / 512;
+    return n < 1 ? 1 : (int)n;
+}
+
+// Whether these kernels take the call, and how they cut it: from more than
+// `from` rows of a sample on average.
+inline bool cut_many(const ams_attn *at, int32_t B, int64_t n_q, int64_t keys, int from, Cut &c)
+{
+    const int64_t Hk = at->n_kv_heads, rows = n_q * (at->n_heads / Hk), samples = B < 1 ? 1 : B;
+    if (rows <= from * samples) return false;
+    int64_t busy = (rows + kManyRows - 1) >> kManyShift;
+    if (busy < samples) busy = samples;
+    c.nsplit = split_many(busy * Hk, keys);
+    c.tiles = tiles_of(rows, kManyShift, B);
+    c.blocks = c.tiles * Hk * c.nsplit;
+    return true;
 }
 
 }  // namespace

@@ -226,7 +226,10 @@ def test_tokens_with_nowhere_to_go():
     (2, 2, 32, 128, [129, 127], [20, 37]),
     (1, 8, 128, 64, [4000], [1]),
     (3, 1, 100, 16, [40, 700], [3, 0]),
-    (8, 4, 128, 16, [90, 5], [1, 1])])
+    (8, 4, 128, 16, [90, 5], [1, 1]),
+    # many rows a sample: one tile and several, of keys too, widths that fill none
+    (2, 4, 64, 32, [700, 0, 64], [40, 30, 33]), (1, 2, 128, 16, [65, 1, 300], [129, 20, 64]),
+    (1, 1, 32, 64, [1500], [200]), (2, 1, 80, 128, [200, 129], [70, 300]), (1, 4, 16, 16, [63, 900], [50, 3])])
 def test_attention(Hk, G, D, page, lens, q_len, dtype):
     c = Cache(len(lens), Hk, D, page, -(-max(lens) // page) + 1, seed=D + page)
     c.write(lens)
