@@ -567,13 +567,15 @@ typedef struct {
  *       not used), other rows left as they were.  k and v being one array, the
  *       gradient is dk + dv.  dq, dk, dv must not overlap anything.
  * Arithmetic: float32 products and sums for AMS_F32; for AMS_BF16 exact bf16
- *       products with float32 sums, the softmax in float32, and one rounding to
- *       bf16 of the weights (of their gradients) before the second product.
+ *       products with float32 sums, the softmax in float32.  The weights (and
+ *       their gradients) enter the second product as a pair of bf16 values,
+ *       within 2^-17, or, where samples have more than 32 rows of queries and
+ *       heads on average (16 for heads wider than 64), rounded to bf16 once.
  * ws:   at least ams_xattn_workspace(attn, B, n_q, n_k) bytes, for either call.
  * Host errors: NULL, DTYPE, DIMS (heads, head_dim), SIZE (a negative size,
- * n_q * n_heads / n_kv_heads or n_k above 2^31 - 1, a stride below the width
- * or above 2^24,
- * more than 2^24 - 1 tiles of 16 rows or 64 keys in all), WORKSPACE. */
+ * n_q * n_heads / n_kv_heads or n_k above 2^30, a stride below the width or
+ * above 2^24, or more work than a grid holds: B * n_kv_heads, or n_kv_heads times
+ * the tiles of 16 rows or 64 keys, above 2^24 - 1), WORKSPACE. */
 size_t ams_xattn_workspace(const ams_attn *attn, int32_t B, int64_t n_q, int64_t n_k);
 ams_status ams_xattn_fwd(const ams_attn *attn, int32_t B, const int32_t *q_off, int64_t n_q, const int32_t *k_off,
                          int64_t n_k, const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v,
@@ -597,8 +599,8 @@ typedef struct {
     int32_t n_kv_heads;  /* 1..4096 */
     int32_t head_dim;    /* 1..128 */
     int32_t page;        /* tokens of a page: 16, 32, 64 or 128 */
-    int32_t max_pages;   /* pages of a sample: columns of the page table (max_pages * page < 2^31) */
-    int64_t n_pages;     /* pages of the pool */
+    int32_t max_pages;   /* pages of a sample: columns of the page table (max_pages * page <= 2^30) */
+    int64_t n_pages;     /* pages of the pool, below 2^31 */
 } ams_cache;
 
 /* write: appends each sample's new tokens behind its start[i] tokens.
@@ -623,7 +625,7 @@ typedef struct {
  *       DIMS).  Codes enter the products exactly.  lse may be NULL.
  *       ws: at least ams_cache_workspace(attn, cache, B, n_q) bytes.
  * Host errors: NULL, DTYPE, DIMS (heads, head_dim, page), SIZE (as for
- * ams_xattn_fwd; n_new, max_pages or n_pages out of range), WORKSPACE. */
+ * ams_xattn_fwd; n_new above 2^30, max_pages or n_pages out of range), WORKSPACE. */
 ams_status ams_cache_write(const ams_cache *cache, int32_t dtype, int32_t B, const int32_t *new_off, int64_t n_new,
                            const int32_t *start, const int32_t *page_table, const void *k, int64_t ld_k,
                            const void *v, int64_t ld_v, uint8_t *k_codes, float *k_scale, uint8_t *v_codes,

@@ -569,7 +569,8 @@ ams_status plan_of(const ams_attn *at, int32_t B, int64_t n_q, int64_t n_k, bool
     const ams_status s = attn_shape(at);
     if (s != AMS_OK) return s;
     const int64_t G = at->n_heads / at->n_kv_heads, Hk = at->n_kv_heads;
-    if (B < 0 || n_q < 0 || n_k < 0 || n_q * G > INT32_MAX || n_k > INT32_MAX) return AMS_ERR_SIZE;
+    if (B < 0 || n_q < 0 || n_k < 0 || n_q > kAttnMaxEntries || n_q * G > kAttnMaxEntries || n_k > kAttnMaxEntries)
+        return AMS_ERR_SIZE;
     const int64_t samples = B < 1 ? 1 : B, rows = n_q * G, keys = n_k / samples;
     p.fwd = p.dq = cut_rows(at, B, n_q, keys, wide);
     // from more rows than attn_bwd_few_k's tile holds (512 samples of 200 keys, 4 heads of 64, forward + backward:

@@ -783,6 +783,7 @@ template <class T> void launch_join(const char *name, const AttnArgs &a, hipStre
 
 constexpr int64_t kAttnMaxBlocks = (1ll << 24) - 1;    // x 256 threads: below the grid's 2^32
 constexpr int kAttnMaxDim = 128;
+constexpr int64_t kAttnMaxEntries = 1 << 30;           // rows or keys: a step past the last one still fits 32 bits
 
 inline ams_status attn_shape(const ams_attn *at)
 {

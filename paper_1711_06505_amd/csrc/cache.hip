@@ -165,7 +165,7 @@ ams_status cache_shape(const ams_cache *c, int &page_shift)
         (1 << page_shift) != c->page)
         return AMS_ERR_DIMS;
     if (c->max_pages < 1 || c->n_pages < 1 || c->n_pages > INT32_MAX ||
-        (int64_t)c->max_pages * c->page > INT32_MAX)
+        (int64_t)c->max_pages * c->page > kAttnMaxEntries)
         return AMS_ERR_SIZE;
     return AMS_OK;
 }
@@ -179,7 +179,8 @@ ams_status read_plan(const ams_attn *at, const ams_cache *c, int32_t B, int64_t 
     if (s == AMS_OK) s = cache_shape(c, shift);
     if (s != AMS_OK) return s;
     if (at->n_kv_heads != c->n_kv_heads || at->head_dim != c->head_dim) return AMS_ERR_DIMS;
-    if (B < 0 || n_q < 0 || n_q * (at->n_heads / at->n_kv_heads) > INT32_MAX) return AMS_ERR_SIZE;
+    if (B < 0 || n_q < 0 || n_q > kAttnMaxEntries || n_q * (at->n_heads / at->n_kv_heads) > kAttnMaxEntries)
+        return AMS_ERR_SIZE;
     cut = cut_rows(at, B, n_q, (int64_t)c->max_pages * c->page, wide);
     // (128 samples of 2000..4000 tokens, 2 key heads of 128, 4 query heads each: 178 us at 80 rows against 183 with
     // it, 336 at 160 rows against 198; 64 wide: 102 against 127 and 159 against 135)
@@ -206,7 +207,7 @@ extern "C" ams_status ams_cache_write(const ams_cache *cache, int32_t dtype, int
     const ams_status s = cache_shape(cache, a.page_shift);
     if (s != AMS_OK) return s;
     const int64_t w = (int64_t)cache->n_kv_heads * cache->head_dim;
-    if (B < 0 || n_new < 0 || n_new > INT32_MAX || ld_k < w || ld_v < w) return AMS_ERR_SIZE;
+    if (B < 0 || n_new < 0 || n_new > kAttnMaxEntries || ld_k < w || ld_v < w) return AMS_ERR_SIZE;
     a.tiles = (n_new >> a.page_shift) + 2ll * B;
     const int64_t waves = a.tiles * cache->n_kv_heads * 2, blocks = (waves + kAttnWaves - 1) / kAttnWaves;
     if (blocks > kAttnMaxBlocks) return AMS_ERR_SIZE;

@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void lookup_bwd_k(int D, int nv, int roun
         const int kk = perm[p];
         if (kk < 0 || kk >= n) return -1;
         const int u = inv[kk];
-        if (u < 0 || u >= cap) return -1;
+        if (u < 0 || u >= cap || u >= n) return -1;
         if (!(pad_id >= 0 && uniq[u] == pad_id)) k = kk;
         return u;
     };
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(kThreads) void lookup_join_k(int D, int nv, int64_t
     const int ka = perm[p1 - 1], kb = perm[p1];
     if (ka < 0 || ka >= n || kb < 0 || kb >= n) return;
     const int u = inv[ka];
-    if (u < 0 || u >= cap || inv[kb] != u) return;
+    if (u < 0 || u >= cap || u >= n || inv[kb] != u) return;
     const int64_t s = uniq_off[u], e1 = uniq_off[u + 1];
     if (s < chunk * C || s >= p1 || e1 <= p1 || e1 > n) return;
     const int64_t last = (e1 - 1) / C;
