@@ -8,7 +8,10 @@
 // with one owner per result and no atomics: dQ's blocks own row tiles and
 // stream keys as the forward does; dK's and dV's own keys, 16 a wave, and
 // stream the rows (all heads of the group), so both their contractions have
-// the operand layouts of the forward with rows and keys exchanged.
+// the operand layouts of the forward with rows and keys exchanged.  Where a
+// sample's rows fit one tile (a few ads against a long list: bound by reading
+// the keys and writing their gradients) a third kernel does all in one pass.
+// bf16 samples of many rows, bound by the products, have attn_many.h's kernels.
 #include <initializer_list>
 
 #include "attn_device.h"
@@ -575,7 +578,10 @@ ams_status plan_of(const ams_attn *at, int32_t B, int64_t n_q, int64_t n_k, bool
     p.fwd = p.dq = cut_rows(at, B, n_q, keys, wide);
     // from more rows than attn_bwd_few_k's tile holds (512 samples of 200 keys, 4 heads of 64, forward + backward:
     // 35 + 48 us at 32 rows against 39 + 136 with attn_many.h, 48 + 176 at 48 rows against 42 + 119)
-    p.many = wide && at->dtype == AMS_BF16 && cut_many(at, B, n_q, keys, at->head_dim <= 64 ? 32 : 16, p.fwd);
+    // and from 64 keys: with fewer the weights' rounding there shows next to the output's (dQ and dK off by 2.7e-3 at 8
+    // keys, 2.4e-3 from 64 on, 1.9e-3 with pairs)
+    p.many = at->dtype == AMS_BF16 && keys >= 64 &&
+             cut_many(at, B, n_q, keys, at->head_dim <= 64 ? 32 : 16, p.fwd);
     if (p.many) p.dq = p.fwd;
     // one pass over the keys where most samples' rows fit one tile
     p.few_rt = wide && at->head_dim <= 64 && rows > 8 * samples ? 2 : 1;
@@ -658,10 +664,10 @@ extern "C" ams_status ams_xattn_fwd(const ams_attn *attn, int32_t B, const int32
     return with_attn(attn->dtype, a.D, pb, [&](auto t, auto dh, auto piece) {
         using T = decltype(t);
         constexpr int DH = decltype(dh)::value, PB = decltype(piece)::value;
-        if constexpr (PB == 16 && sizeof(T) == 2) {
+        if constexpr (sizeof(T) == 2) {
             if (pl.many) {
                 AMS_LAUNCH("xattn_fwd_many", st,
-                           attn_fwd_many_k<DH, false><<<(unsigned)pl.fwd.blocks, kAttnThreads, 0, st>>>(a));
+                           attn_fwd_many_k<DH, PB, false><<<(unsigned)pl.fwd.blocks, kAttnThreads, 0, st>>>(a));
                 if (a.nsplit > 1) launch_join<T>("xattn_join", a, st);
                 return ams_launch_status();
             }
@@ -718,18 +724,18 @@ extern "C" ams_status ams_xattn_bwd(const ams_attn *attn, int32_t B, const int32
                        attn_sum_k<T><<<(unsigned)(blocks < 8192 ? blocks : 8192), kAttnThreads, 0, st>>>(
                            a.part_o, a.nsplit, per, heads, a.D, off, B, n, (T *)x0, ld0, (T *)x1, ld1));
         };
-        if constexpr (PB == 16 && sizeof(T) == 2) {
+        if constexpr (sizeof(T) == 2) {
             if (pl.many) {
                 if (n_q > 0) {
                     a.nsplit = pl.dq.nsplit, a.tiles = pl.dq.tiles;
                     AMS_LAUNCH("xattn_dq_many", st,
-                               attn_dq_many_k<DH><<<(unsigned)pl.dq.blocks, kAttnThreads, 0, st>>>(a));
+                               attn_dq_many_k<DH, PB><<<(unsigned)pl.dq.blocks, kAttnThreads, 0, st>>>(a));
                     if (a.nsplit > 1) sum(1, a.H, q_off, n_q, dq, ld_dq, nullptr, 0);
                 }
                 if (n_k > 0) {
                     a.nsplit = pl.dkv, a.tiles = pl.key_tiles;
                     AMS_LAUNCH("xattn_dkv_many", st,
-                               attn_dkv_many_k<DH><<<(unsigned)(pl.key_tiles * a.Hk * a.nsplit), kAttnThreads, 0, st>>>(a));
+                               attn_dkv_many_k<DH, PB><<<(unsigned)(pl.key_tiles * a.Hk * a.nsplit), kAttnThreads, 0, st>>>(a));
                     if (a.nsplit > 1) sum(2, a.Hk, k_off, n_k, dk, ld_dk, dv, ld_dv);
                 }
                 return ams_launch_status();

@@ -131,51 +131,65 @@ __device__ __forceinline__ Work many_work(int64_t b, const AttnArgs &a)
 // themselves, lane by lane, so the permutation is made on the source side.
 // What lies behind D or behind the last row reads another piece of the tile:
 // the first meets zeros of the other operand or results that nobody stores,
-// the second weights of zero.
-template <int DH, int N = kManyStep> struct Dma {
+// the second weights of zero.  Rows that are not aligned to 16 bytes (PB < 16)
+// come through registers, in loads of PB bytes.
+template <int DH, int PB, int N = kManyStep> struct Dma {
     using TL = Tile<DH, N>;
-    uint32_t off[TL::kPer];
+    uint32_t off[TL::kPer];                            // of the row; with 16-byte pieces of the piece in it
 
     __device__ static __forceinline__ int slot(int i)
     {
         return (__builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE) * TL::kPer + i) * AMS_WAVE + ams_lane();
     }
     __device__ static __forceinline__ int row(int i) { return slot(i) / TL::kPieces; }
+    __device__ static __forceinline__ int piece(int i) { return (slot(i) % TL::kPieces) ^ TL::swizzle(row(i)); }
     __device__ static __forceinline__ uint32_t col(int i, int D)
     {
-        const int r = row(i), piece = (slot(i) % TL::kPieces) ^ TL::swizzle(r);
-        return piece * 8 < D ? piece * 16 : 0;
+        return PB == 16 && piece(i) * 8 < D ? piece(i) * 16 : 0;
     }
     __device__ __forceinline__ void rows(int last, uint32_t ld, int D)        // of a plain list
     {
 #pragma unroll
         for (int i = 0; i < TL::kPer; ++i) off[i] = (uint32_t)min(row(i), last) * ld + col(i, D);
     }
-    __device__ __forceinline__ void issue(const char *base, char *tile) const
+    __device__ __forceinline__ void issue(const char *base, char *tile, int D) const
     {
-        char *t = tile + __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE) * TL::kPer * 1024;
+        if constexpr (PB == 16) {
+            char *t = tile + __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE) * TL::kPer * 1024;
 #pragma unroll
-        for (int i = 0; i < TL::kPer; ++i)
-            __builtin_amdgcn_global_load_lds(base + off[i], (lds_bytes *)(t + i * 1024), 16, 0, 0);
+            for (int i = 0; i < TL::kPer; ++i)
+                __builtin_amdgcn_global_load_lds(base + off[i], (lds_bytes *)(t + i * 1024), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < TL::kPer; ++i) {
+                uint4 v;
+                Cols<uint16_t, 8, PB>(piece(i) * 8, D).load((uint32_t *)&v, base, off[i]);
+                *(uint4 *)(tile + slot(i) * 16) = v;
+            }
+        }
     }
 };
 
 // A list's rows into a tile that stays, with zeros behind D; there after the next barrier.
-template <int DH, int N>
+template <int DH, int PB, int N>
 __device__ __forceinline__ void stage_rows(const char *base, int last, uint32_t ld, int D, char *tile)
 {
-    Dma<DH, N> dma;
+    Dma<DH, PB, N> dma;
     dma.rows(last, ld, D);
-    dma.issue(base, tile);
+    dma.issue(base, tile, D);
     if (D == DH) return;
     staged();
-    for (int i = threadIdx.x; i < N * (DH / 8); i += kAttnThreads)
-        if (i % (DH / 8) * 8 >= D) *(uint4 *)(tile + Tile<DH, N>::at(i / (DH / 8), i % (DH / 8))) = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < N * DH / 2; i += kAttnThreads) {           // words
+        const int r = i / (DH / 2), d = i % (DH / 2) * 2;
+        uint32_t *w = (uint32_t *)(tile + Tile<DH, N>::at(r, d / 8)) + d % 8 / 2;
+        if (d >= D) *w = 0;
+        else if (d + 1 == D) *w &= 0xffffu;
+    }
 }
 
 // The keys' side: 64 of K and V a step ahead.
-template <int DH> struct KeyStage {
-    Dma<DH> k, v;
+template <int DH, int PB> struct KeyStage {
+    Dma<DH, PB> k, v;
     uint32_t byte;                                     // the lane's key's mask byte
 
     __device__ __forceinline__ explicit KeyStage(const AttnArgs &a)
@@ -191,8 +205,8 @@ template <int DH> struct KeyStage {
             v.rows(last, (uint32_t)(a.ld_v * 2), a.D);
         }
         byte = a.mask ? a.mask[k0 + kb + min(ams_lane(), last)] : 1;
-        k.issue((const char *)a.k + ((int64_t)(k0 + kb) * a.ld_k + (int64_t)h * a.D) * 2, kt);
-        v.issue((const char *)a.v + ((int64_t)(k0 + kb) * a.ld_v + (int64_t)h * a.D) * 2, vt);
+        k.issue((const char *)a.k + ((int64_t)(k0 + kb) * a.ld_k + (int64_t)h * a.D) * 2, kt, a.D);
+        v.issue((const char *)a.v + ((int64_t)(k0 + kb) * a.ld_v + (int64_t)h * a.D) * 2, vt, a.D);
     }
     // The tile of the keys from kb on is there: which of them take part.  Masked ones become zeros.
     __device__ __forceinline__ uint64_t arrive(const AttnArgs &a, int kb, int hi, char *kt, char *vt)
@@ -273,8 +287,8 @@ template <int DH> struct PageStage {
 };
 
 // The rows' side: N of Q and dO a step ahead, with their log-sum-exp and delta.
-template <int DH, int N> struct RowStage {
-    using DM = Dma<DH, N>;
+template <int DH, int PB, int N> struct RowStage {
+    using DM = Dma<DH, PB, N>;
     DM q, d;
     float lse, delta;
     bool same = false;                                 // the offsets of a whole step hold for the next one
@@ -299,13 +313,13 @@ template <int DH, int N> struct RowStage {
         const int64_t at = ((int64_t)q0 + n) * a.H + h * a.G + (r - n * a.G);
         lse = a.lse[at];
         delta = a.delta[at];
-        q.issue((const char *)a.q + (query * a.ld_q + (int64_t)h * a.G * a.D) * 2, qt);
-        d.issue((const char *)a.dout + (query * a.ld_dout + (int64_t)h * a.G * a.D) * 2, dt);
+        q.issue((const char *)a.q + (query * a.ld_q + (int64_t)h * a.G * a.D) * 2, qt, a.D);
+        d.issue((const char *)a.dout + (query * a.ld_dout + (int64_t)h * a.G * a.D) * 2, dt, a.D);
     }
 };
 
-// The wave's 32 rows as operand.
-template <int DH>
+// The wave's 32 rows as operand, with zeros behind D.
+template <int DH, int PB>
 __device__ __forceinline__ void rows_frag(Frag *f, const void *x, int64_t ld, const Row &row, int D)
 {
     const char *p = (const char *)x + (row.query * ld + (int64_t)row.head * D) * 2;
@@ -313,20 +327,22 @@ __device__ __forceinline__ void rows_frag(Frag *f, const void *x, int64_t ld, co
 #pragma unroll
     for (int c = 0; c < DH / 16; ++c) {
         const int d = 16 * c + 8 * hh;
-        *(uint4 *)f[c].u = *(const uint4 *)(p + (d < D ? d * 2 : 0));
-        if (d >= D) *(uint4 *)f[c].u = make_uint4(0, 0, 0, 0);
+        const Cols<uint16_t, 8, PB> cols(d, D);
+        cols.load(f[c].u, p, 0);
+        if (D < DH) cols.mask(f[c].u, d, D);
     }
 }
 
 // Four consecutive values of a result row.
-__device__ __forceinline__ void store4(void *row, int d, int D, float a, float b, float c, float e)
+template <int PB> __device__ __forceinline__ void store4(void *row, int d, int D, float a, float b, float c, float e)
 {
-    if (d < D) *(uint2 *)((char *)row + d * 2) = make_uint2(pack_bf16(a, b), pack_bf16(c, e));
+    const float v[4] = {a, b, c, e};
+    store_elems<uint16_t, 4, PB>((uint16_t *)row, d, D, v);
 }
 
 // ---------------------------------------------------------------- forward
 
-template <int DH, bool PAGED> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_many_k(AttnArgs a)
+template <int DH, int PB, bool PAGED> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_many_k(AttnArgs a)
 {
     using TL = Tile<DH>;
     constexpr int NC = DH / 16, ND = DH / 32;
@@ -355,7 +371,7 @@ template <int DH, bool PAGED> __global__ __launch_bounds__(kAttnThreads, 2) void
     split_range(nk, wk.split, a.nsplit, lo, hi);
 
     Frag qf[NC];
-    rows_frag<DH>(qf, a.q, a.ld_q, row, a.D);
+    rows_frag<DH, PB>(qf, a.q, a.ld_q, row, a.D);
     // a positive factor, so that the maximum can be taken before it: a negative scale goes onto Q's signs
     const float c = fmaxf(fabsf(a.scale) * kLog2e, 1.2e-38f);
     if (a.scale < 0.f) {
@@ -369,7 +385,7 @@ template <int DH, bool PAGED> __global__ __launch_bounds__(kAttnThreads, 2) void
     for (int d = 0; d < ND; ++d) acc[d] = zero16();
     float mx = kNegInf, l = 0.f;
     take_turns();
-    typename std::conditional<PAGED, PageStage<DH>, KeyStage<DH>>::type st(a);
+    typename std::conditional<PAGED, PageStage<DH>, KeyStage<DH, PB>>::type st(a);
     auto step = [&](int kb, char *kt, char *vt, char *kn, char *vn) {
         uint64_t live;
         float sk[4] = {c, c, c, c}, sv[4] = {1.f, 1.f, 1.f, 1.f};
@@ -468,14 +484,14 @@ template <int DH, bool PAGED> __global__ __launch_bounds__(kAttnThreads, 2) void
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
-            store4(out, 32 * d + entry_of(r, hh), a.D, acc[d][r] * inv, acc[d][r + 1] * inv, acc[d][r + 2] * inv,
+            store4<PB>(out, 32 * d + entry_of(r, hh), a.D, acc[d][r] * inv, acc[d][r + 1] * inv, acc[d][r + 2] * inv,
                    acc[d][r + 3] * inv);
     if (a.lse && hh == 0) a.lse[at] = l == 0.f ? kNegInf : (mx + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // -------------------------------------------------------------- dQ, delta
 
-template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_many_k(AttnArgs a)
+template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_many_k(AttnArgs a)
 {
     using TL = Tile<DH>;
     constexpr int NC = DH / 16, ND = DH / 32;
@@ -496,12 +512,12 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_man
     split_range(k1 > k0 ? k1 - k0 : 0, wk.split, a.nsplit, lo, hi);
 
     Frag qf[NC], df[NC];
-    rows_frag<DH>(qf, a.q, a.ld_q, row, a.D);
-    rows_frag<DH>(df, a.dout, a.ld_dout, row, a.D);
+    rows_frag<DH, PB>(qf, a.q, a.ld_q, row, a.D);
+    rows_frag<DH, PB>(df, a.dout, a.ld_dout, row, a.D);
     float delta = 0.f;
     {
         Frag of[NC];
-        rows_frag<DH>(of, a.o, a.ld_o, row, a.D);
+        rows_frag<DH, PB>(of, a.o, a.ld_o, row, a.D);
 #pragma unroll
         for (int x = 0; x < NC; ++x)
 #pragma unroll
@@ -521,7 +537,7 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_man
 #pragma unroll
     for (int d = 0; d < ND; ++d) acc[d] = zero16();
     take_turns();
-    KeyStage<DH> st(a);
+    KeyStage<DH, PB> st(a);
     auto step = [&](int kb, char *kt, char *vt, char *kn, char *vn) {
         const uint64_t live = st.arrive(a, kb, hi, kt, vt);
         if (kb + kManyStep < hi) st.issue(a, h, k0, kb + kManyStep, hi, kn, vn);
@@ -573,7 +589,7 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_man
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
-            store4(dq, 32 * d + entry_of(r, hh), a.D, acc[d][r], acc[d][r + 1], acc[d][r + 2], acc[d][r + 3]);
+            store4<PB>(dq, 32 * d + entry_of(r, hh), a.D, acc[d][r], acc[d][r + 1], acc[d][r + 2], acc[d][r + 3]);
 }
 
 // ----------------------------------------------------------------- dK, dV
@@ -582,7 +598,7 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dq_man
 // Both sums of a wave are 2 DH registers.  For two waves per SIMD at DH = 128
 // the values stay in shared memory, read anew for each tile, and a tile is 32
 // rows (8 x 1536 queries, 16 heads, 3072 keys: 867 us; one wave per SIMD with all in registers: 1125).
-template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_many_k(AttnArgs a)
+template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_many_k(AttnArgs a)
 {
     constexpr bool kShared = DH == 128;
     constexpr int N = kShared ? 32 : 64;
@@ -607,13 +623,13 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_ma
     const uint64_t all_live = ams_ballot(live_key);
 
     Frag kf[NC], vf[kShared ? 1 : NC];
-    rows_frag<DH>(kf, a.k, a.ld_k, Row{key, h}, a.D);
+    rows_frag<DH, PB>(kf, a.k, a.ld_k, Row{key, h}, a.D);
     if constexpr (kShared) {
         const char *vp = (const char *)a.v + ((keys.begin + keys.first) * a.ld_v + (int64_t)h * a.D) * 2;
         const int64_t left = keys.count - 1 - keys.first;
-        stage_rows<DH, kManyRows>(vp, (int)(left < kManyRows - 1 ? left : kManyRows - 1), (uint32_t)(a.ld_v * 2), a.D, s_v);
+        stage_rows<DH, PB, kManyRows>(vp, (int)(left < kManyRows - 1 ? left : kManyRows - 1), (uint32_t)(a.ld_v * 2), a.D, s_v);
     } else {
-        rows_frag<DH>(vf, a.v, a.ld_v, Row{key, h}, a.D);
+        rows_frag<DH, PB>(vf, a.v, a.ld_v, Row{key, h}, a.D);
     }
     const float c = a.scale * kLog2e;
     f32x16 ak[ND], av[ND];
@@ -627,7 +643,7 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_ma
         const int bits = __builtin_amdgcn_readfirstlane((int)__float_as_uint(a.lse[w.query * a.H + w.head]));
         if (__uint_as_float((uint32_t)bits) == kNegInf) hi = lo;
     }
-    RowStage<DH, N> st;
+    RowStage<DH, PB, N> st;
     take_turns();
     auto step = [&](int rb, char *qt, char *dt, char *qn, char *dn, int buf) {
         if (wave == 0 && lane < N) {
@@ -698,8 +714,8 @@ template <int DH> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_ma
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
-            store4(dk, 32 * d + entry_of(r, hh), a.D, ak[d][r], ak[d][r + 1], ak[d][r + 2], ak[d][r + 3]);
-            store4(dv, 32 * d + entry_of(r, hh), a.D, av[d][r], av[d][r + 1], av[d][r + 2], av[d][r + 3]);
+            store4<PB>(dk, 32 * d + entry_of(r, hh), a.D, ak[d][r], ak[d][r + 1], ak[d][r + 2], ak[d][r + 3]);
+            store4<PB>(dv, 32 * d + entry_of(r, hh), a.D, av[d][r], av[d][r + 1], av[d][r + 2], av[d][r + 3]);
         }
 }
 

@@ -293,7 +293,7 @@ extern "C" ams_status ams_cache_attn(const ams_attn *attn, const ams_cache *cach
         if constexpr (PB == 16 && sizeof(T) == 2) {
             if (many) {
                 AMS_LAUNCH("cache_attn_many", st,
-                           attn_fwd_many_k<DH, true><<<(unsigned)cut.blocks, kAttnThreads, 0, st>>>(a));
+                           attn_fwd_many_k<DH, PB, true><<<(unsigned)cut.blocks, kAttnThreads, 0, st>>>(a));
                 if (a.nsplit > 1) launch_join<T>("cache_join", a, st);
                 return ams_launch_status();
             }

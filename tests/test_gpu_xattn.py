@@ -142,6 +142,14 @@ def test_many_rows(shape, drop):
         Problem(*shape, "f32", drop=drop, seed=14).check()
 
 
+@pytest.mark.parametrize("D,extra,offset", [(89, 0, 0), (33, 3, 1), (12, 4, 4), (100, 0, 2), (127, 1, 0), (64, 1, 3)])
+def test_many_rows_of_any_alignment(D, extra, offset):
+    p = Problem([150, 40], [130, 260], 4, 2, D, "bf16", drop=0.2, extra=extra, offset=offset, seed=16)
+    p.k[p.mask == 0] = float("nan")
+    p.v[p.mask == 0] = float("nan")
+    p.check()
+
+
 def test_many_rows_without_a_key():
     """Every key of one sample masked: zero rows, whatever the upstream gradient holds there."""
     p = Problem([100, 80], [90, 70], 2, 1, 64, "bf16", seed=15, drop=0.1)
