@@ -87,22 +87,31 @@ template <int DH, int N = kManyStep> struct Tile {
     {
         return (uint32_t)(row * kRowBytes + ((piece ^ swizzle(row)) << 4));
     }
-    // rows `row0` + lane % 32 as operand of a contraction over the width, piece 2 c + lane / 32
-    __device__ static __forceinline__ Frag row_frag(const char *t, int row0, int c)
+    // The permutation is an exclusive or on the piece's bits, so a lane keeps one offset for all its row reads and
+    // one for its transposed reads; a piece further, or eight rows, is another bit.
+    __device__ static __forceinline__ uint32_t row_base()
     {
-        const int lane = ams_lane(), row = row0 + (lane & 31);
+        return at(ams_lane() & 31, ams_lane() >> 5);
+    }
+    __device__ static __forceinline__ uint32_t col_base()
+    {
+        const int lane = ams_lane(), i = lane & 15;
+        return at(4 * (lane >> 5) + (i >> 2), 2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) + (i & 1) * 8;
+    }
+    // rows `row0` + lane % 32 as operand of a contraction over the width, piece 2 c + lane / 32
+    __device__ static __forceinline__ Frag row_frag(const char *t, uint32_t base, int row0, int c)
+    {
         Frag f;
-        *(uint4 *)f.u = *(const uint4 *)(t + at(row, 2 * c + (lane >> 5)));
+        *(uint4 *)f.u = *(const uint4 *)(t + (base ^ (uint32_t)(c << 5)) + row0 * kRowBytes);
         return f;
     }
     // operand of output columns 32 dt + lane % 32 for the contraction over rows row0 .. row0 + 15
-    __device__ static __forceinline__ Frag col_frag(const char *t, int row0, int dt)
+    __device__ static __forceinline__ Frag col_frag(const char *t, uint32_t base, int row0, int dt)
     {
-        const int lane = ams_lane(), i = lane & 15;
-        const int row = row0 + 4 * (lane >> 5) + (i >> 2), piece = 4 * dt + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+        const uint32_t at = base ^ (uint32_t)(dt << 6);
         Frag f;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(t + at(row, piece) + (i & 1) * 8));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(t + at(row + 8, piece) + (i & 1) * 8));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(t + at + row0 * kRowBytes));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(t + (at ^ 32u) + (row0 + 8) * kRowBytes));
         *(s16x4 *)&f.u[0] = lo;
         *(s16x4 *)&f.u[2] = hi;
         return f;
@@ -385,6 +394,7 @@ template <int DH, int PB, bool PAGED> __global__ __launch_bounds__(kAttnThreads,
     for (int d = 0; d < ND; ++d) acc[d] = zero16();
     float mx = kNegInf, l = 0.f;
     take_turns();
+    const uint32_t row_at_lane = TL::row_base(), col_at_lane = TL::col_base();
     typename std::conditional<PAGED, PageStage<DH>, KeyStage<DH, PB>>::type st(a);
     auto step = [&](int kb, char *kt, char *vt, char *kn, char *vn) {
         uint64_t live;
@@ -405,7 +415,7 @@ template <int DH, int PB, bool PAGED> __global__ __launch_bounds__(kAttnThreads,
 #pragma unroll
         for (int x = 0; x < NC; ++x)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) s[t] = mma32(TL::row_frag(kt, 32 * t, x), qf[x], s[t]);
+            for (int t = 0; t < 2; ++t) s[t] = mma32(TL::row_frag(kt, row_at_lane, 32 * t, x), qf[x], s[t]);
         if constexpr (PAGED) {                         // a page's scale: registers 8 g .. 8 g + 7 are 16 tokens
 #pragma unroll
             for (int r = 0; r < 32; ++r) s[r >> 4][r & 15] *= sk[r >> 3];
@@ -446,7 +456,7 @@ template <int DH, int PB, bool PAGED> __global__ __launch_bounds__(kAttnThreads,
             for (int x = 0; x < 2; ++x) {
                 const Frag p = pack16(s[t], x);
 #pragma unroll
-                for (int d = 0; d < ND; ++d) acc[d] = mma32(TL::col_frag(vt, 32 * t + 16 * x, d), p, acc[d]);
+                for (int d = 0; d < ND; ++d) acc[d] = mma32(TL::col_frag(vt, col_at_lane, 32 * t + 16 * x, d), p, acc[d]);
             }
     };
     if (lo < hi) {
@@ -537,6 +547,7 @@ template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void att
 #pragma unroll
     for (int d = 0; d < ND; ++d) acc[d] = zero16();
     take_turns();
+    const uint32_t row_at_lane = TL::row_base(), col_at_lane = TL::col_base();
     KeyStage<DH, PB> st(a);
     auto step = [&](int kb, char *kt, char *vt, char *kn, char *vn) {
         const uint64_t live = st.arrive(a, kb, hi, kt, vt);
@@ -546,8 +557,8 @@ template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void att
             f32x16 s = zero16(), dp = zero16();
 #pragma unroll
             for (int x = 0; x < NC; ++x) {
-                s = mma32(TL::row_frag(kt, 32 * t, x), qf[x], s);
-                dp = mma32(TL::row_frag(vt, 32 * t, x), df[x], dp);
+                s = mma32(TL::row_frag(kt, row_at_lane, 32 * t, x), qf[x], s);
+                dp = mma32(TL::row_frag(vt, row_at_lane, 32 * t, x), df[x], dp);
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -563,7 +574,7 @@ template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void att
             for (int x = 0; x < 2; ++x) {
                 const Frag p = pack16(s, x);
 #pragma unroll
-                for (int d = 0; d < ND; ++d) acc[d] = mma32(TL::col_frag(kt, 32 * t + 16 * x, d), p, acc[d]);
+                for (int d = 0; d < ND; ++d) acc[d] = mma32(TL::col_frag(kt, col_at_lane, 32 * t + 16 * x, d), p, acc[d]);
             }
         }
     };
@@ -597,7 +608,7 @@ template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void att
 // 128 keys a block, 32 a wave; rows in tiles with their log-sum-exp and delta.
 // Both sums of a wave are 2 DH registers.  For two waves per SIMD at DH = 128
 // the values stay in shared memory, read anew for each tile, and a tile is 32
-// rows (8 x 1536 queries, 16 heads, 3072 keys: 867 us; one wave per SIMD with all in registers: 1125).
+// rows (8 x 1536 queries, 16 heads, 3072 keys: 745 us; one wave per SIMD with all in registers: 1125).
 template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_many_k(AttnArgs a)
 {
     constexpr bool kShared = DH == 128;
@@ -645,6 +656,7 @@ template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void att
     }
     RowStage<DH, PB, N> st;
     take_turns();
+    const uint32_t row_at_lane = TL::row_base(), col_at_lane = TL::col_base();
     auto step = [&](int rb, char *qt, char *dt, char *qn, char *dn, int buf) {
         if (wave == 0 && lane < N) {
             s_lse[buf][lane] = rb + lane < hi ? st.lse * kLog2e : -kNegInf;
@@ -657,9 +669,9 @@ template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void att
             f32x16 s = zero16(), dp = zero16();
 #pragma unroll
             for (int x = 0; x < NC; ++x) {
-                s = mma32(TL::row_frag(qt, 32 * t, x), kf[x], s);
-                if constexpr (kShared) dp = mma32(TL::row_frag(dt, 32 * t, x), VT::row_frag(s_v, 32 * wave, x), dp);
-                else dp = mma32(TL::row_frag(dt, 32 * t, x), vf[x], dp);
+                s = mma32(TL::row_frag(qt, row_at_lane, 32 * t, x), kf[x], s);
+                if constexpr (kShared) dp = mma32(TL::row_frag(dt, row_at_lane, 32 * t, x), VT::row_frag(s_v, row_at_lane, 32 * wave, x), dp);
+                else dp = mma32(TL::row_frag(dt, row_at_lane, 32 * t, x), vf[x], dp);
             }
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
@@ -684,8 +696,8 @@ template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void att
                 const Frag p = pack16(s, x), ds = pack16(dp, x);
 #pragma unroll
                 for (int d = 0; d < ND; ++d) {
-                    av[d] = mma32(TL::col_frag(dt, 32 * t + 16 * x, d), p, av[d]);
-                    ak[d] = mma32(TL::col_frag(qt, 32 * t + 16 * x, d), ds, ak[d]);
+                    av[d] = mma32(TL::col_frag(dt, col_at_lane, 32 * t + 16 * x, d), p, av[d]);
+                    ak[d] = mma32(TL::col_frag(qt, col_at_lane, 32 * t + 16 * x, d), ds, ak[d]);
                 }
             }
         }
