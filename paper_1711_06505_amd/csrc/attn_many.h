@@ -41,7 +41,7 @@ __device__ __forceinline__ void staged()
 // alike they fall into step, both in their products and then both in their
 // exponentials; with one of them (by its slot) always first, the other one
 // fills in what it leaves free (364 and 512 us without, 353 and 495 with, forward
-// and dQ of 8 x 1536 queries, 16 heads of 128, 3072 keys).
+// and dQ of 8 samples of 1024..2048 queries and 2048..4096 keys, 16 heads of 128).
 __device__ __forceinline__ void take_turns()
 {
     if (__builtin_amdgcn_s_getreg((3 << 11) | 4) & 1) __builtin_amdgcn_s_setprio(1);
@@ -608,7 +608,8 @@ template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void att
 // 128 keys a block, 32 a wave; rows in tiles with their log-sum-exp and delta.
 // Both sums of a wave are 2 DH registers.  For two waves per SIMD at DH = 128
 // the values stay in shared memory, read anew for each tile, and a tile is 32
-// rows (8 x 1536 queries, 16 heads, 3072 keys: 745 us; one wave per SIMD with all in registers: 1125).
+// rows (8 samples of 1024..2048 queries and 2048..4096 keys, 16 heads: 745 us;
+// one wave per SIMD with all in registers: 1125).
 template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void attn_dkv_many_k(AttnArgs a)
 {
     constexpr bool kShared = DH == 128;
