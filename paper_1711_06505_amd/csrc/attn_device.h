@@ -640,30 +640,16 @@ __global__ __launch_bounds__(kAttnThreads, (waves_per_simd<T, DH, RT>())) void a
 
 #pragma unroll
     for (int t = 0; t < RT; ++t) l[t] = sum_groups(l[t]);
-    const int64_t n_rows = a.n_q * a.H;
     if constexpr (WK == 1) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             if (rows.first + 16 * t + m >= R) continue;
             const int64_t at = row[t].query * a.H + row[t].head;
-            float o[4 * VD];
-            if (a.nsplit > 1) {
-                const int64_t p = (int64_t)wk.split * n_rows + at;
-                acc_in_order<VD>(acc[t], 1.f, o);
-#pragma unroll
-                for (int i = 0; i < 4 * VD; ++i)
-                    if (4 * g * VD + i < a.D) a.part_o[p * a.D + 4 * g * VD + i] = o[i];
-                if (g == 0) {
-                    a.part_ml[2 * p] = mx[t];
-                    a.part_ml[2 * p + 1] = l[t];
-                }
-            } else {
-                acc_in_order<VD>(acc[t], l[t] == 0.f ? 0.f : 1.f / l[t], o);      // no key: a zero row
-                store_elems<T, 4 * VD, PB>((T *)a.out + row[t].query * a.ld_out + (int64_t)row[t].head * a.D,
-                                           4 * g * VD, a.D, o);
-                if (a.lse && g == 0)
-                    a.lse[at] = l[t] == 0.f ? kNegInf : (mx[t] + __builtin_amdgcn_logf(l[t])) * kLn2;
-            }
+            float o[4 * VD];                          // one split where a wave has a tile of its own
+            acc_in_order<VD>(acc[t], l[t] == 0.f ? 0.f : 1.f / l[t], o);          // no key: a zero row
+            store_elems<T, 4 * VD, PB>((T *)a.out + row[t].query * a.ld_out + (int64_t)row[t].head * a.D, 4 * g * VD,
+                                       a.D, o);
+            if (a.lse && g == 0) a.lse[at] = l[t] == 0.f ? kNegInf : (mx[t] + __builtin_amdgcn_logf(l[t])) * kLn2;
         }
         return;
     }
@@ -701,7 +687,7 @@ __global__ __launch_bounds__(kAttnThreads, (waves_per_simd<T, DH, RT>())) void a
         const Row ow = row_at(a, rows.begin, h, (int)ro);
         const int64_t at = ow.query * a.H + ow.head;
         if (a.nsplit > 1) {
-            const int64_t p = (int64_t)wk.split * n_rows + at;
+            const int64_t p = (int64_t)wk.split * (a.n_q * a.H) + at;
             if (threadIdx.x % 16 == 0) {
                 a.part_ml[2 * p] = M;
                 a.part_ml[2 * p + 1] = L;
