@@ -557,7 +557,8 @@ typedef struct {
  *       and keys, non-decreasing within [0, n_q] and [0, n_k]; rows that no
  *       sample owns are neither read nor written.
  *       q, out [n_q x n_heads x head_dim], k, v [n_k x n_kv_heads x head_dim],
- *       row strides ld_* >= the heads' width.  k and v may be the same array.
+ *       row strides ld_* >= the heads' width.  k and v may be the same array;
+ *       out and lse must not overlap anything.
  *       key_mask [n_k] bytes, or NULL: a key whose byte is 0 takes no part,
  *       whatever its k and v rows hold (NaN included).
  *       lse [n_q x n_heads] out, or NULL for inference: ln sum_j e^(s_j).

@@ -330,7 +330,7 @@ __global__ __launch_bounds__(kAttnThreads, (DH == 128 ? 1 : waves_per_simd<T, DH
 {
     if (blockIdx.x == gridDim.x - 1) {
         bool found = false;
-#pragma unroll 4
+#pragma unroll 16
         for (int s = threadIdx.x; s < a.B; s += kAttnThreads)
             found |= (int64_t)(clamp_off(a.q_off[s + 1], a.n_q) - clamp_off(a.q_off[s], a.n_q)) * a.G > a.few_rows;
         const int any = __syncthreads_or(found);

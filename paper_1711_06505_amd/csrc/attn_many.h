@@ -269,7 +269,8 @@ template <int DH> struct PageStage {
     }
     __device__ __forceinline__ uint64_t arrive(int kb, int hi, char *kt, char *vt)
     {
-        there = there_next, ks = ks_next, vs = vs_next;
+        // a token without a page: zeros, whatever the scales that were read in its place
+        there = there_next, ks = there ? ks_next : 1.f, vs = there ? vs_next : 0.f;
         const uint64_t live = ams_ballot(there && kb + ams_lane() < hi);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
@@ -416,10 +417,6 @@ template <int DH, int PB, bool PAGED> __global__ __launch_bounds__(kAttnThreads,
         for (int x = 0; x < NC; ++x)
 #pragma unroll
             for (int t = 0; t < 2; ++t) s[t] = mma32(TL::row_frag(kt, row_at_lane, 32 * t, x), qf[x], s[t]);
-        if constexpr (PAGED) {                         // a page's scale: registers 8 g .. 8 g + 7 are 16 tokens
-#pragma unroll
-            for (int r = 0; r < 32; ++r) s[r >> 4][r & 15] *= sk[r >> 3];
-        }
         if (live != ~0ull) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -428,12 +425,15 @@ template <int DH, int PB, bool PAGED> __global__ __launch_bounds__(kAttnThreads,
                     if (!(live >> (32 * t + entry_of(r, hh)) & 1)) s[t][r] = kNegInf;
         }
         // the running maximum may lag by 2^8: weights stay below 2^8, and the sums are rescaled that much less often
-        float tm = kNegInf;
+        float tm = kNegInf;                            // of each 16 keys, which have one positive factor
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int g = 0; g < 4; ++g) {
+            float m = s[g >> 1][8 * (g & 1)];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) tm = fmaxf(tm, s[t][r]);
-        tm = fmaxf(tm, __shfl_xor(tm, 32, AMS_WAVE)) * (PAGED ? 1.f : c);
+            for (int r = 1; r < 8; ++r) m = fmaxf(m, s[g >> 1][8 * (g & 1) + r]);
+            tm = fmaxf(tm, m * sk[g]);
+        }
+        tm = fmaxf(tm, __shfl_xor(tm, 32, AMS_WAVE));
         if (ams_ballot(tm > mx + 8.f)) {
             const float mn = fmaxf(mx, tm), alpha = __builtin_amdgcn_exp2f(mx - (mn == kNegInf ? 0.f : mn));
             mx = mn;
@@ -446,9 +446,9 @@ template <int DH, int PB, bool PAGED> __global__ __launch_bounds__(kAttnThreads,
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[t][r] = __builtin_amdgcn_exp2f(PAGED ? s[t][r] - base : s[t][r] * c - base);
+                s[t][r] = __builtin_amdgcn_exp2f(s[t][r] * sk[2 * t + (r >> 3)] - base);
                 l += s[t][r];
-                if constexpr (PAGED) s[t][r] = s[t][r] == 0.f ? 0.f : s[t][r] * sv[2 * t + (r >> 3)];
+                if constexpr (PAGED) s[t][r] *= sv[2 * t + (r >> 3)];          // a power of two: exact
             }
 #pragma unroll
         for (int t = 0; t < 2; ++t)
