@@ -417,13 +417,14 @@ struct Work {
     int split, h;
     int64_t tile;
 };
-__device__ __forceinline__ Work work_of(int64_t b, const AttnArgs &a)
+__device__ __forceinline__ Work work_of(int64_t at, const AttnArgs &a)
 {
+    uint32_t b = (uint32_t)at;                         // below 4 kAttnMaxBlocks
     Work w;
-    w.split = (int)(b % a.nsplit);
-    b /= a.nsplit;
-    w.h = (int)(b % a.Hk);
-    w.tile = b / a.Hk;
+    w.split = (int)(b % (uint32_t)a.nsplit);
+    b /= (uint32_t)a.nsplit;
+    w.h = (int)(b % (uint32_t)a.Hk);
+    w.tile = b / (uint32_t)a.Hk;
     return w;
 }
 

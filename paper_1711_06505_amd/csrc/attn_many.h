@@ -121,18 +121,19 @@ template <int DH, int N = kManyStep> struct Tile {
 // Block of the work, so that neighbouring tiles (of one sample and key head,
 // which read the same keys) run on one XCD and share its cache: hardware deals
 // the blocks out to the 8 XCDs in turn.
-__device__ __forceinline__ int64_t xcd_block()
+__device__ __forceinline__ uint32_t xcd_block()
 {
-    const int64_t b = blockIdx.x, per = gridDim.x / 8;
+    const uint32_t b = blockIdx.x, per = gridDim.x / 8;
     return b < per * 8 ? (b % 8) * per + b / 8 : b;
 }
-__device__ __forceinline__ Work many_work(int64_t b, const AttnArgs &a)
+__device__ __forceinline__ Work many_work(uint32_t b, const AttnArgs &a)
 {
+    const uint32_t tiles = (uint32_t)a.tiles;
     Work w;
-    w.tile = b % a.tiles;
-    b /= a.tiles;
-    w.split = (int)(b % a.nsplit);
-    w.h = (int)(b / a.nsplit);
+    w.tile = b % tiles;
+    b /= tiles;
+    w.split = (int)(b % (uint32_t)a.nsplit);
+    w.h = (int)(b / (uint32_t)a.nsplit);
     return w;
 }
 

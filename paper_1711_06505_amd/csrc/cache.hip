@@ -78,12 +78,12 @@ template <class T, int N>
 __global__ __launch_bounds__(kAttnThreads) void cache_write_k(WriteArgs a)
 {
     const int lane = ams_lane();
-    int64_t w = (int64_t)blockIdx.x * kAttnWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);
+    uint32_t w = blockIdx.x * kAttnWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / AMS_WAVE);     // below 2^26
     if (w >= a.tiles * a.Hk * 2) return;
     const int kv = (int)(w & 1);
     w >>= 1;
-    const int h = (int)(w % a.Hk);
-    const int64_t tile = w / a.Hk;
+    const int h = (int)(w % (uint32_t)a.Hk);
+    const int64_t tile = w / (uint32_t)a.Hk;
     const int i = find_sample(a.new_off, a.B, a.n_new, 1, a.page_shift, 2, tile);
     const int n0 = clamp_off(a.new_off[i], a.n_new), n1 = clamp_off(a.new_off[i + 1], a.n_new);
     const int64_t start = a.start[i], P = 1ll << a.page_shift;
