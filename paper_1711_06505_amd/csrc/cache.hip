@@ -17,22 +17,26 @@ namespace {
 constexpr float kCodeMax = 448.f;                     // largest e4m3 value, 1.75 2^8
 constexpr int kMinExp = -100;                         // of a scale: 2^kMinExp and its inverse are normal
 
-// Four elements of a row as floats.
-template <class T, int N> __device__ __forceinline__ void load_f32(float *x, const T *p)
-{
-    if constexpr (N == 4) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 v = *(const float4 *)p;
-            x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+// N (4 or 1) elements of a row, as they lie there and as floats.
+template <class T, int N> struct Elems {
+    typedef typename std::conditional<N == 1, T, typename std::conditional<sizeof(T) == 4, uint4, uint2>::type>::type raw;
+    raw r;
+
+    __device__ __forceinline__ void load(const T *p) { r = *(const raw *)p; }
+    __device__ __forceinline__ void floats(float *x) const
+    {
+        if constexpr (N == 1) {
+            if constexpr (sizeof(T) == 4) x[0] = r;
+            else x[0] = ams_bf16_to_f32(r);
+        } else if constexpr (sizeof(T) == 4) {
+            x[0] = __uint_as_float(r.x), x[1] = __uint_as_float(r.y);
+            x[2] = __uint_as_float(r.z), x[3] = __uint_as_float(r.w);
         } else {
-            const uint2 v = *(const uint2 *)p;
-            x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
-            x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
+            x[0] = __uint_as_float(r.x << 16), x[1] = __uint_as_float(r.x & 0xffff0000u);
+            x[2] = __uint_as_float(r.y << 16), x[3] = __uint_as_float(r.y & 0xffff0000u);
         }
-    } else {
-        x[0] = sizeof(T) == 4 ? *(const float *)p : ams_bf16_to_f32(*(const uint16_t *)p);
     }
-}
+};
 
 // Round to e4m3, ties to even; beyond the largest value: that value (infinities too), NaN stays NaN.
 __device__ __forceinline__ float into_range(float x)
@@ -72,8 +76,10 @@ struct WriteArgs {
 
 // One wave per (page that a sample's new tokens touch, key head, keys or
 // values): the new tokens' largest magnitude, the page's scale, the codes
-// that were there in the new scale where it grew, the new codes.  The new
-// rows are read twice, the second time from the caches; bound by memory.
+// that were there in the new scale where it grew, the new codes.  Bound by
+// memory: the new rows stay in registers between the two, up to kHold pieces a
+// lane (1024 pieces of 4 entries); a larger page's are read again.
+constexpr int kHold = 16;
 template <class T, int N>
 __global__ __launch_bounds__(kAttnThreads) void cache_write_k(WriteArgs a)
 {
@@ -99,16 +105,35 @@ __global__ __launch_bounds__(kAttnThreads) void cache_write_k(WriteArgs a)
     }
     const int rows = (int)(hi - lo), in = (int)(lo - pi * P), per = a.D / N, units = rows * per;
     const T *x = (const T *)a.x[kv] + (n0 + (lo - start)) * a.ld[kv] + (int64_t)h * a.D;
-    uint32_t most = 0;
-#pragma unroll 4
-    for (int u = lane; u < units; u += AMS_WAVE) {
+    auto load = [&](Elems<T, N> &v, int u) {
         const int r = u / per, c = u - r * per;
+        v.load(x + r * a.ld[kv] + c * N);
+    };
+    uint32_t most = 0;
+    auto look = [&](const Elems<T, N> &e) {
         float v[N];
-        load_f32<T, N>(v, x + r * a.ld[kv] + c * N);
+        e.floats(v);
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const uint32_t b = __float_as_uint(v[e]) & 0x7fffffffu;
+        for (int i = 0; i < N; ++i) {
+            const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
             most = b < 0x7f800000u && b > most ? b : most;      // an infinity saturates, NaN stays
+        }
+    };
+    const bool held = units <= kHold * AMS_WAVE;
+    Elems<T, N> hold[kHold];
+    if (held) {
+#pragma unroll
+        for (int i = 0; i < kHold; ++i)
+            if (i * AMS_WAVE < units) load(hold[i], min(i * AMS_WAVE + lane, units - 1));
+#pragma unroll
+        for (int i = 0; i < kHold; ++i)
+            if (i * AMS_WAVE < units) look(hold[i]);
+    } else {
+#pragma unroll 4
+        for (int u = lane; u < units; u += AMS_WAVE) {
+            Elems<T, N> v;
+            load(v, u);
+            look(v);
         }
     }
 #pragma unroll
@@ -144,14 +169,24 @@ __global__ __launch_bounds__(kAttnThreads) void cache_write_k(WriteArgs a)
     if (lane == 0) a.scale[kv][at] = s;
     const float f = 1.f / s;
     codes += (int64_t)in * a.D;
-#pragma unroll 4
-    for (int u = lane; u < units; u += AMS_WAVE) {
-        const int r = u / per, c = u - r * per;
+    auto put = [&](const Elems<T, N> &e, int u) {
         float v[N];
-        load_f32<T, N>(v, x + r * a.ld[kv] + c * N);
+        e.floats(v);
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] *= f;
+        for (int i = 0; i < N; ++i) v[i] *= f;
         store_codes<N>(codes + (int64_t)u * N, v);
+    };
+    if (held) {
+#pragma unroll
+        for (int i = 0; i < kHold; ++i)
+            if (i * AMS_WAVE + lane < units) put(hold[i], i * AMS_WAVE + lane);
+    } else {
+#pragma unroll 4
+        for (int u = lane; u < units; u += AMS_WAVE) {
+            Elems<T, N> v;
+            load(v, u);
+            put(v, u);
+        }
     }
 }
 
