@@ -237,6 +237,20 @@ def test_attention(Hk, G, D, page, lens, q_len, dtype):
     c.attend(q_len, Hk * G, dtype, extra=3, with_lse=False)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("offset,D,q", [(1, 64, 2), (4, 64, 2), (8, 32, 50), (16, 128, 50), (2, 12, 1)])
+def test_pools_at_any_address(offset, D, q, dtype):
+    c = Cache(2, 2, D, 16, 8, seed=offset)
+    for i in range(2):
+        x = c.dev[i]
+        c.dev[i] = torch.zeros(x.numel() + offset, dtype=torch.uint8, device="cuda")[offset:].view(x.shape)
+        c.dev[i].copy_(x)
+    c.write([100, 37], dtype)
+    c.write([1, 20], dtype)
+    c.check()
+    c.attend([q, q + 1], 4, dtype)
+
+
 def test_lengths_beyond_the_table_and_unwritten_slots():
     """A length is taken as max_pages pages at most; what unwritten slots hold
     (NaN codes) does not count."""

@@ -204,6 +204,15 @@ def test_training_step_of_a_table_in_a_graph():
             assert torch.equal(x[:rows_of], y[:rows_of]), k
 
 
+def test_gradient_twice_is_the_same():
+    """Fixed orders: the same bits again, hot rows over many chunks included."""
+    rng = np.random.default_rng(9)
+    ids = torch.from_numpy(make_ids("zipf", 150_000, 700, rng)).cuda()
+    x = torch.from_numpy(rng.standard_normal((150_000, 24)).astype(np.float32)).cuda()
+    first, again = (backward(ids, 700, x, 1.5, -1, 24)[1] for _ in range(2))
+    np.testing.assert_array_equal(first, again)
+
+
 def test_on_another_stream():
     rng = np.random.default_rng(8)
     T = torch.from_numpy(rng.standard_normal((100, 16)).astype(np.float32)).cuda()

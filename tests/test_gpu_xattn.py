@@ -198,6 +198,16 @@ def test_many_short_samples(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [12, 64, 128])
+def test_one_large_sample_among_small_ones(D, dtype):
+    """Gradients of samples of few rows and of the others come from different
+    kernels of one call; with few samples also in several shares of the keys."""
+    Problem([1] * 30 + [90, 0, 2], [25] * 15 + [0] * 5 + [7] * 10 + [150, 9, 60], 4, 2, D, dtype, seed=17).check()
+    Problem([1, 25], [3000, 500], 2, 2, D, dtype, drop=0.1, seed=18).check()
+    Problem([35, 1], [40, 2500], 2, 1, D, dtype, seed=19).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_large_scores(dtype):
     """Scores of several hundred: the maximum is what keeps the softmax finite."""
     Problem([9], [150], 2, 1, 64, dtype, seed=4, spread=8.0).check()
@@ -265,6 +275,27 @@ def test_captured_graph(dtype):
         torch.cuda.synchronize()
         for a, b in zip(buf, (out, lse, *grads)):
             assert torch.equal(a[:5], b[:5]), k
+
+
+@pytest.mark.parametrize("q_len,k_len", [([3, 1, 2], [40, 70, 9]), ([90, 70], [130, 100])])
+def test_rows_before_the_first_sample(q_len, k_len):
+    """Offsets that begin behind 0: the rows in front are nobody's, and the
+    samples' results are what they are without them."""
+    a = Problem(q_len, k_len, 4, 2, 32, "bf16", seed=20)
+    b = Problem([5] + q_len, [7] + k_len, 4, 2, 32, "bf16", seed=20)
+    nq, nk = sum(q_len), sum(k_len)
+    for x, y, lead, n in ((a.q, b.q, 5, nq), (a.do, b.do, 5, nq), (a.k, b.k, 7, nk), (a.v, b.v, 7, nk)):
+        y[lead:lead + n] = x[:n]
+        y[:lead] = float("nan")
+    b.q_off, b.k_off = b.q_off[1:].contiguous(), b.k_off[1:].contiguous()
+    b.q_len, b.k_len = q_len, k_len
+    res = []
+    for p in (a, b):
+        out, lse = p.forward()
+        res.append((out, *p.backward(out, lse)))
+    for x, y, lead, n in zip(*res, (5, 5, 7, 7), (nq, nq, nk, nk)):
+        assert torch.equal(x[:n], y[lead:lead + n])
+        assert (y[:lead] == -3.0).all() and (y[lead + n:] == -3.0).all()
 
 
 def test_two_streams_at_once():
