@@ -353,6 +353,11 @@ template <int PB> __device__ __forceinline__ void store4(void *row, int d, int D
 
 // ---------------------------------------------------------------- forward
 
+// A factor of scores that is not zero, so that the -infinity of an entry that
+// takes no part stays one under it.  The least float32 (2^-149) stands for
+// zero: it moves no weight by more than 2^-21, whatever the product.
+__device__ __forceinline__ float above_zero(float x) { return fmaxf(x, 1.4e-45f); }
+
 template <int DH, int PB, bool PAGED> __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_many_k(AttnArgs a)
 {
     using TL = Tile<DH>;
@@ -384,7 +389,7 @@ template <int DH, int PB, bool PAGED> __global__ __launch_bounds__(kAttnThreads,
     Frag qf[NC];
     rows_frag<DH, PB>(qf, a.q, a.ld_q, row, a.D);
     // a positive factor, so that the maximum can be taken before it: a negative scale goes onto Q's signs
-    const float c = fmaxf(fabsf(a.scale) * kLog2e, 1.2e-38f);
+    const float c = fabsf(a.scale) * kLog2e, c0 = above_zero(c);
     if (a.scale < 0.f) {
 #pragma unroll
         for (int x = 0; x < NC; ++x)
@@ -400,11 +405,11 @@ template <int DH, int PB, bool PAGED> __global__ __launch_bounds__(kAttnThreads,
     typename std::conditional<PAGED, PageStage<DH>, KeyStage<DH, PB>>::type st(a);
     auto step = [&](int kb, char *kt, char *vt, char *kn, char *vn) {
         uint64_t live;
-        float sk[4] = {c, c, c, c}, sv[4] = {1.f, 1.f, 1.f, 1.f};
+        float sk[4] = {c0, c0, c0, c0}, sv[4] = {1.f, 1.f, 1.f, 1.f};
         if constexpr (PAGED) {
             live = st.arrive(kb, hi, kt, vt);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) sk[g] = c * st.of(st.ks, g), sv[g] = st.of(st.vs, g);
+            for (int g = 0; g < 4; ++g) sk[g] = above_zero(c * st.of(st.ks, g)), sv[g] = st.of(st.vs, g);
             if (kb + kManyStep < hi) {
                 st.issue(a, h, kb + kManyStep, hi);
                 if (kb + 2 * kManyStep < hi) st.find(a, pages, kb + 2 * kManyStep, hi);
