@@ -479,6 +479,7 @@ template <int DH, int PB, bool PAGED> __global__ __launch_bounds__(kAttnThreads,
         if (kb + kManyStep < hi) step(kb + kManyStep, s_k1, s_v1, s_k0, s_v0);
     }
     l += __shfl_xor(l, 32, AMS_WAVE);
+    if (c != c && l != 0.f) l = c;                     // a scale that is NaN, which above_zero took out
     if (r_mine >= R) return;
     const int64_t at = row.query * a.H + row.head;
     if (a.nsplit > 1) {

@@ -72,3 +72,18 @@ def test_zero_scale_over_large_entries(q):
     c.write([70], make=lambda r, s: np.sign(r.standard_normal(s)) * 2.0 ** 100)
     rows = torch.from_numpy(np.sign(c.rng.standard_normal((q, 1, 64))) * 2.0 ** 60)
     attend(c, [q], 1, "bf16", 0.0, rows)
+
+
+@pytest.mark.parametrize("q", [2, 150])
+def test_a_scale_that_is_not_a_number(q):
+    """NaN goes through to every row that attends to something."""
+    c = Cache(1, 1, 64, 16, 5, seed=q)
+    c.write([70])
+    off = torch.tensor([0, q], dtype=torch.int32, device="cuda")
+    x = torch.ones((q, 1, 64), dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros_like(x)
+    attn = ams.make_attn(1, 1, 64, "bf16", float("nan"))
+    ws = torch.empty(ams.ams_cache_workspace(attn, c.cache, 1, q), dtype=torch.uint8, device="cuda")
+    ams.ams_cache_attn(attn, c.cache, off, torch.from_numpy(c.len).cuda(), torch.from_numpy(c.table).cuda(), x,
+                       *c.arrays(), out, ws)
+    assert torch.isnan(out).all()

@@ -1,5 +1,5 @@
-"""A scale of zero for few and many rows: equal weights, whatever the products
-are (up to 2^126 here)."""
+"""Scales of the scores at the ends of their range, for few and many rows: zero
+over products up to 2^126 (equal weights all the same), and NaN."""
 import pytest
 import torch
 
@@ -24,3 +24,14 @@ def test_zero_over_large_products(q, dtype):
         tol = ((live[keys, None] * v.abs()).sum(0) / n) * 1.1 * (2 * (2.0 ** -8 if dtype == "bf16" else 0) + (n + 20) * 2.0 ** -24)
         assert ((out[rows].double() - want).abs() <= tol).all()
         assert ((lse[rows].double() - torch.log(torch.tensor(n).double())).abs() <= (n + 20) * 2.0 ** -24 * 6).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("q", [2, 150])
+def test_not_a_number(q, dtype):
+    """NaN goes through to every row that attends to something, and to no other one."""
+    p = Problem([q, 3], [130, 0], 2, 1, 64, dtype, seed=q)
+    p.attn.scale = float("nan")
+    out, lse = p.forward()
+    assert torch.isnan(out[:q]).all() and torch.isnan(lse[:q]).all()
+    assert (out[q:q + 3] == 0).all() and (out[q + 3:] == -3.0).all()
