@@ -510,7 +510,12 @@ ams_status ams_adam_update(int64_t n, float *param, const float *grad, float *m,
  * (ams_bag_fwd keeps only their sum), and multi-head attention of a sample's
  * queries to its own list.  `dtype` is AMS_F32 or AMS_BF16 (else DTYPE), the
  * storage of the rows that go in and come out; sums, softmax statistics and
- * the row gradients of a table are float32.  Row strides (ld_*) are in elements. */
+ * the row gradients of a table are float32.  Row strides (ld_*) are in elements.
+ * Bits:  how a call is cut, and with it the order of its sums, follows its
+ * counts, its widths and dtype, and which of 16, 8, 4 and 2 bytes divide the
+ * addresses and strides of its arrays.  The same call on buffers aligned alike
+ * gives the same bits; a sample in another batch, or a buffer aligned
+ * otherwise, may differ by roundings. */
 
 /* ------------------------------------------------------------ lookup ----
  * out[k][d] = scale * table[ids[k]][d]   for k < n, d < D (1 <= D <= 65536).
@@ -524,7 +529,11 @@ ams_status ams_adam_update(int64_t n, float *param, const float *grad, float *m,
  *       zero for uniq[u] == pad_id; grad [n_uniq_cap x D] float32, written for
  *       u < n_u (what ams_adagrad_rows takes).  dout [n x D] in dtype, row
  *       stride ld_dout >= D.  A row's tokens are added in an order that depends
- *       on n and on their places in the sorted order alone.
+ *       on their places in the sorted order, on n, D and dtype, and on how dout,
+ *       its stride and grad are aligned.  inv alone says which rows there are;
+ *       *n_uniq is not read.  IDs outside the table have no place in a sorted
+ *       order (ams_dedup: ID_RANGE): a batch that holds such needs them set to
+ *       pad_id first.
  *       ws: at least ams_lookup_workspace(n, D) bytes; that size also serves
  *       every smaller n.
  * Host errors: DTYPE, DIMS (D), SIZE (n outside [0, 2^30 - 1], n_rows < 0, a
