@@ -580,8 +580,8 @@ typedef struct {
  *       products with float32 sums, the softmax in float32.  The weights (and
  *       their gradients) enter the second product as a pair of bf16 values,
  *       within 2^-17, or, where samples have more than 32 rows of queries and
- *       heads on average (16 for heads wider than 64) and 64 keys, rounded to
- *       bf16 once.
+ *       a key head's query heads on average (16 for heads wider than 64) and
+ *       at least 64 keys, rounded to bf16 once (within 2^-8).
  * ws:   at least ams_xattn_workspace(attn, B, n_q, n_k) bytes, for either call.
  * Host errors: NULL, DTYPE, DIMS (heads, head_dim), SIZE (a negative size,
  * n_q * n_heads / n_kv_heads or n_k above 2^30, a stride below the width or
@@ -633,10 +633,19 @@ typedef struct {
  *       lengths[i] tokens of sample i's pages (at most max_pages * page of them;
  *       several samples may share pages).  Tokens of a page outside [0, n_pages)
  *       take no part.  attn and cache agree in n_kv_heads and head_dim (else
- *       DIMS).  Codes enter the products exactly.  lse may be NULL.
+ *       DIMS).  Codes enter the products exactly; for AMS_BF16 the weights as a
+ *       pair within 2^-17, or, where samples have more than 96 rows of queries
+ *       and a key head's query heads on average, head_dim is a multiple of 16
+ *       and q, out, their strides and the codes are aligned to 16 bytes, rounded
+ *       to bf16 once (within 2^-8).  lse may be NULL.  A NaN among the first
+ *       lengths[i] tokens leaves sample i's results in its key head unspecified.
+ *       Long histories are cut into shares by what a sample can hold, max_pages
+ *       * page tokens, as the lengths are only known on the device: a table much
+ *       wider than its users costs empty shares, in time and workspace.
  *       ws: at least ams_cache_workspace(attn, cache, B, n_q) bytes.
- * Host errors: NULL, DTYPE, DIMS (heads, head_dim, page), SIZE (as for
- * ams_xattn_fwd; n_new above 2^30, max_pages or n_pages out of range), WORKSPACE. */
+ * Host errors: NULL, DTYPE, DIMS (heads, head_dim, page), SIZE (a negative size,
+ * n_new or n_q * n_heads / n_kv_heads above 2^30, max_pages or n_pages out of
+ * range, a stride below the width, or more work than a grid holds), WORKSPACE. */
 ams_status ams_cache_write(const ams_cache *cache, int32_t dtype, int32_t B, const int32_t *new_off, int64_t n_new,
                            const int32_t *start, const int32_t *page_table, const void *k, int64_t ld_k,
                            const void *v, int64_t ld_v, uint8_t *k_codes, float *k_scale, uint8_t *v_codes,

@@ -793,8 +793,9 @@ struct Cut {
 // launched (each sample's own number is not known here).
 inline int64_t tiles_of(int64_t n, int shift, int32_t B) { return (n >> shift) + B; }
 
-// Splits of the streamed side when `tiles` blocks have work: up to two blocks
-// per compute unit while a split keeps 256 entries (two steps of the block;
+// Splits of the streamed side when `tiles` blocks have work and a list has
+// `entries` (over pages: room for them, which a sample may fill less): up to two
+// blocks per compute unit while a split keeps 256 entries (two steps of the block;
 // below that its partial sums cost more than it saves), up to four with 1536
 // (measured: 3 queries over 80,000 keys, 8 heads of 128, 188 us at 21 splits
 // and 171 at 42; 32 queries over 2,300 8-bit tokens, 8 key heads, 51 us at 2
