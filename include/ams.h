@@ -569,7 +569,9 @@ typedef struct {
  *       row strides ld_* >= the heads' width.  k and v may be the same array;
  *       out and lse must not overlap anything.
  *       key_mask [n_k] bytes, or NULL: a key whose byte is 0 takes no part,
- *       whatever its k and v rows hold (NaN included).
+ *       whatever its k and v rows hold (NaN included).  Other rows that hold an
+ *       infinity or NaN leave the results of their own sample and key head
+ *       unspecified, and no other's.
  *       lse [n_q x n_heads] out, or NULL for inference: ln sum_j e^(s_j).
  * bwd:  the same inputs, the forward's out and lse, and dout [n_q x n_heads x
  *       head_dim]; dq, dk, dv like q, k, v: fully overwritten on the samples'
