@@ -13,7 +13,7 @@
 // eight consecutive rows fall on different banks either way.
 //
 // Weights and their gradients are rounded to bf16 once before the second
-// product (relative 2^-9 at most, their sums are not rounded): a pair as in
+// product (relative 2^-8 at most, their sums are not rounded): a pair as in
 // attn_device.h would add half of the second product's instructions here.
 #pragma once
 
