@@ -469,6 +469,12 @@ class _Call:
             self._refuse(name, t, dtype, None)
         return t.data_ptr(), ld
 
+    def matrix(self, name, t):
+        """Rows and width of a table of rows."""
+        if t.dim() != 2:
+            raise ValueError(f"{self.where}: {name} is {tuple(t.shape)}, [rows, width] needed")
+        return t.shape
+
     def storage(self, name, t) -> int:
         if t.dtype not in _STORAGE:
             raise ValueError(f"{self.where}: {name} must be float32 or bfloat16, not {t.dtype}")
@@ -496,12 +502,12 @@ class _Call:
 def ams_lookup_fwd(ids, table, out, scale: float = 1.0, pad_id: int = -1, stream=None):
     """out[k] = scale * table[ids[k]] (float32 or bfloat16 rows, any row stride)."""
     c = _Call("ams_lookup_fwd", ids)
-    n, D = ids.numel(), table.shape[1]
+    n, (n_rows, D) = ids.numel(), c.matrix("table", table)
     dt = c.storage("table", table)
     ip = c.vec("ids", ids, torch.int32, n)
     tp, ldt = c.rows("table", table, table.dtype, 0, (D,))
     op, ldo = c.rows("out", out, table.dtype, n, (D,))
-    c.run(load().ams_lookup_fwd, dt, D, float(scale), int(pad_id), ip, n, tp, table.shape[0], ldt, op, ldo,
+    c.run(load().ams_lookup_fwd, dt, D, float(scale), int(pad_id), ip, n, tp, n_rows, ldt, op, ldo,
           stream=stream)
 
 
@@ -514,7 +520,7 @@ def ams_lookup_bwd(uniq, inv, occ_perm, uniq_off, n_uniq, n_uniq_cap: int, dout,
     """grad[u] = scale * the sum of dout over the tokens of uniq[u], from the
     outputs of ams_dedup over the tokens' IDs (dout has one row per token)."""
     c = _Call("ams_lookup_bwd", dout)
-    n, D = dout.shape
+    n, D = c.matrix("dout", dout)
     dt, i32 = c.storage("dout", dout), torch.int32
     dp, ldd = c.rows("dout", dout, dout.dtype, n, (D,))
     args = [c.vec("uniq", uniq, i32, min(n, n_uniq_cap)), c.vec("inv", inv, i32, n),
