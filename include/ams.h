@@ -583,7 +583,8 @@ typedef struct {
  *       their gradients) enter the second product as a pair of bf16 values,
  *       within 2^-17, or, where samples have more than 32 rows of queries and
  *       a key head's query heads on average (16 for heads wider than 64) and
- *       at least 64 keys, rounded to bf16 once (within 2^-8).
+ *       at least 64 keys, rounded to bf16 once (within 2^-8); on the way to dq of
+ *       heads up to 32 wide always as a pair.
  * ws:   at least ams_xattn_workspace(attn, B, n_q, n_k) bytes, for either call.
  * Host errors: NULL, DTYPE, DIMS (heads, head_dim), SIZE (a negative size,
  * n_q * n_heads / n_kv_heads or n_k above 2^30, a stride below the width or

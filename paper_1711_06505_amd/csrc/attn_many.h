@@ -13,8 +13,15 @@
 // eight consecutive rows fall on different banks either way.
 //
 // Weights and their gradients are rounded to bf16 once before the second
-// product (relative 2^-8 at most, their sums are not rounded): a pair as in
-// attn_device.h would add half of the second product's instructions here.
+// product (relative 2^-8 at most, their sums are not rounded), but for dQ of
+// heads up to 32 wide.  A pair as in attn_device.h everywhere takes the errors
+// against 64 bits (by norm, normal inputs) from 2.2e-3 to 1.7e-3 for outputs and
+// from 2.4e-3 to 1.7e-3 for gradients, where the rounding of the result alone is
+// 1.7e-3, and the time of 8 samples of 1024..2048 queries and 2048..4096 keys, 16
+// heads of 128, from 1.66 to 2.21 ms (forward 360 -> 489, dQ 517 -> 626, dK and dV
+// 777 -> 1086 us).  dQ of narrow heads is off by more, 2.4e-3 at 32, 2.6e-3 at 16
+// and 2.7e-3 at 8 wide: pairs there (1.7e-3, 1.8e-3, 1.9e-3; with heads of 32 the
+// same samples' dQ takes 251 us instead of 195).
 #pragma once
 
 #include "attn_device.h"
@@ -68,6 +75,16 @@ __device__ __forceinline__ Frag pack16(const f32x16 &x, int c)
     Frag f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) f.u[i] = pack_bf16(x[8 * c + 2 * i], x[8 * c + 2 * i + 1]);
+    return f;
+}
+// what that rounding left, rounded
+__device__ __forceinline__ Frag rest16(const f32x16 &x, int c, const Frag &h)
+{
+    Frag f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        f.u[i] = pack_bf16(x[8 * c + 2 * i] - __uint_as_float(h.u[i] << 16),
+                           x[8 * c + 2 * i + 1] - __uint_as_float(h.u[i] & 0xffff0000u));
     return f;
 }
 // entry of register r in lane half hh
@@ -581,7 +598,11 @@ template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void att
             for (int x = 0; x < 2; ++x) {
                 const Frag p = pack16(s, x);
 #pragma unroll
-                for (int d = 0; d < ND; ++d) acc[d] = mma32(TL::col_frag(kt, col_at_lane, 32 * t + 16 * x, d), p, acc[d]);
+                for (int d = 0; d < ND; ++d) {
+                    const Frag k = TL::col_frag(kt, col_at_lane, 32 * t + 16 * x, d);
+                    acc[d] = mma32(k, p, acc[d]);
+                    if constexpr (DH == 32) acc[d] = mma32(k, rest16(s, x, p), acc[d]);
+                }
             }
         }
     };
