@@ -334,9 +334,13 @@ int lanes_of(int nv)
     return L;
 }
 
-// Positions per chunk, in rounds of 64: one round while the chunks are few;
-// four from 131072 tokens on, where a hot row's partial rows are the cost.
-int bwd_rounds(int64_t n) { return n >= 131072 ? 4 : 1; }
+// Positions per chunk, in rounds of 64: one round while the chunks are few, which
+// keeps more waves at work; four where there are enough, which leaves fewer partial
+// rows (with one and with four, us: 32 floats 12 and 17 at 131072 tokens, 18 and 20
+// at 262144, 44 and 39 at 823k, 109 and 89 at 2M; 512 bf16 28 and 61 at 64k,
+// 47 and 64 at 131072, 110 and 101 at 262144).
+constexpr int64_t kFourRounds = 262144;
+int bwd_rounds(int64_t n) { return n >= kFourRounds ? 4 : 1; }
 
 template <class F> ams_status with_lanes(int L, F f)
 {
@@ -406,9 +410,9 @@ extern "C" size_t ams_lookup_workspace(int64_t n, int32_t D)
 {
     if (n < 0 || n > kMaxTok || D < 1 || D > kMaxWidth) return 0;
     // one round per chunk below the switch, so that a smaller n never needs more
-    const int64_t few = n < 131072 ? n : 131071;
+    const int64_t few = n < kFourRounds ? n : kFourRounds - 1;
     const int64_t a = (few + AMS_WAVE - 1) / AMS_WAVE;
-    const int64_t b = n < 131072 ? 0 : (n + 4 * AMS_WAVE - 1) / (4 * AMS_WAVE);
+    const int64_t b = n < kFourRounds ? 0 : (n + 4 * AMS_WAVE - 1) / (4 * AMS_WAVE);
     return (size_t)(a > b ? a : b) * 2 * D * sizeof(float) + 256;
 }
 
