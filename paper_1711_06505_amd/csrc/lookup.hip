@@ -39,8 +39,12 @@ template <class T> __device__ __forceinline__ T from_f32(float x);
 template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
 template <> __device__ __forceinline__ uint16_t from_f32<uint16_t>(float x) { return ams_f32_to_bf16(x); }
 
-// Past the caches: rows of less than a wave's width gain by it (823k x 32
-// float32: 24 us against 32), wider ones lose (64k x 2048 bf16: 88 against 79).
+// Past the caches, which keep what is read again: the table here, the upstream
+// rows in the backward that follows.  Us through the caches and past them, the
+// lookup alone, repeated: 24 and 21 (823k x 32 float32), 24 and 21 (200k x 256
+// bf16), 81 and 59 (64k x 2048 bf16); a step of it with dedup and gradient: 158
+// and 147, 131 and 115, 231 and 218.  With nothing in the caches the lookup itself
+// takes up to 4 % longer.
 template <class T, int N> __device__ __forceinline__ void store_stream(T *p, const Piece<T, N> &x)
 {
     constexpr int B = N * (int)sizeof(T);
@@ -89,8 +93,7 @@ __global__ __launch_bounds__(kThreads) void lookup_fwd_k(int nv, float scale, in
                 if (k >= n) continue;
 #pragma unroll
                 for (int e = 0; e < N; ++e) x[r].e[e] = id[r] >= 0 ? from_f32<T>(to_f32(x[r].e[e]) * scale) : (T)0;
-                if constexpr (L < AMS_WAVE) store_stream(out + k * ld_out + (int64_t)c * N, x[r]);
-                else *(typename Piece<T, N>::raw *)(out + k * ld_out + (int64_t)c * N) = x[r].r;
+                store_stream(out + k * ld_out + (int64_t)c * N, x[r]);
             }
         }
     }
