@@ -794,18 +794,20 @@ struct Cut {
 inline int64_t tiles_of(int64_t n, int shift, int32_t B) { return (n >> shift) + B; }
 
 // Splits of the streamed side when `tiles` blocks have work and a list has
-// `entries` (over pages: room for them, which a sample may fill less): up to two
-// blocks per compute unit while a split keeps 256 entries (two steps of the block;
-// below that its partial sums cost more than it saves), up to four with 1536
-// (measured: 3 queries over 80,000 keys, 8 heads of 128, 188 us at 21 splits
-// and 171 at 42; 32 queries over 2,300 8-bit tokens, 8 key heads, 51 us at 2
-// splits and 53 at 4).
+// `entries` (over pages: room for them, which a sample may fill less): two blocks
+// per compute unit while a split keeps 256 entries (two steps of the block; below
+// that its partial sums cost more than it saves), four where each of them keeps
+// 1200.  Numbers between the two leave units idle at the end.  Us with two and
+// four a unit, at so many entries for each of the four: 8 users of 8,000..16,000
+// 8-bit tokens, 8 key heads of 128, 48 and 50 at 1000 (61 at 10 splits between), 32 of
+// 512..4096 51 and 55 at 1024; one query over 40,000 float32 keys, 8 samples, 4 heads of 64,
+// 145 and 134 at 1250, over 60,000 bf16 keys, 3 samples, 8 heads of 128, 152 and 139 at
+// 1430, over 80,000 188 and 170 at 1900.
 inline int split_count(int64_t tiles, int64_t entries)
 {
     if (tiles < 1) tiles = 1;
-    const int64_t two = 512 / tiles < entries / 256 ? 512 / tiles : entries / 256;
-    const int64_t four = 1024 / tiles < entries / 1536 ? 1024 / tiles : entries / 1536;
-    const int64_t n = two > four ? two : four;
+    const int64_t four = 1024 / tiles, two = 512 / tiles < entries / 256 ? 512 / tiles : entries / 256;
+    const int64_t n = four > two && entries / 1200 >= four ? four : two;
     return n < 1 ? 1 : (n > 256 ? 256 : (int)n);
 }
 
