@@ -763,7 +763,9 @@ template <int DH, int PB> __global__ __launch_bounds__(kAttnThreads, 2) void att
 // ------------------------------------------------------------------- host
 
 // A block of attn_many.h has 128 rows of partial sums to write and join again: a split per compute unit, of 512
-// entries at least.
+// entries at least.  Forward and backward, us at 256, 512 and 1024 entries: 64 queries over 1500 keys, 4 heads of 64,
+// 37, 47 and 61; 2 samples of 1000 over 1500 89, 79 and 83; 16 of 100 queries, 8 heads of 64, over 600 73, 50 and 50.
+// Up to two splits a unit: 8 samples of 128 queries over 12,000 keys, 4 heads of 128, 337 against 289.
 inline int split_many(int64_t tiles, int64_t entries)
 {
     if (tiles < 1) tiles = 1;
