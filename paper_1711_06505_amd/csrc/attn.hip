@@ -1,7 +1,8 @@
 // attn.hip -- multi-head attention of each sample's queries to that sample's
 // keys, two lists of different lengths (the tiles are attn_device.h's).
 //   ams_xattn_fwd  P = softmax(scale Q K^T) over the sample's live keys, O = P V
-//   ams_xattn_bwd  with delta = rowsum(dO o O) and dS = scale P o (dO V^T - delta):
+//   ams_xattn_bwd  with delta = rowsum(dO o O), in bf16 over few keys rowsum(P o dO V^T),
+//                  and dS = scale P o (dO V^T - delta):
 //                  dQ = dS K, dK = dS^T Q, dV = P^T dO, the last two summed over
 //                  the query heads of a key head.
 // The backward forms P again from the forward's log-sum-exp, in two kernels
